@@ -238,7 +238,7 @@ def _plain_logprobs(s):
         order = torch.where(bits < 0, bits ^ 0x7FFFFFFF, bits).long() * (1 << 32) + (c["vocab"] - 1 - torch.arange(c["vocab"], device=x.device))
         ids = c["vocab"] - 1 - (order.topk(c["top_k"], 1).values & 0xFFFFFFFF)
         z = y.gather(1, ids)
-        out["top_ids"] = torch.where(live[:, None], ids, -1).to(torch.int32)
+        out["top_ids"] = torch.where(live[:, None] & ~torch.isneginf(z), ids, -1).to(torch.int32)     # what is ruled out is no alternative
         out["top_logprobs"] = torch.where(live[:, None], torch.where(torch.isneginf(z), z, z - lse[:, None]), 0.0)
     return out
 
@@ -307,7 +307,7 @@ def _to_e4m3(x, bits16, at_least_one):
     tiny = torch.floor(z * 512 + r.float() * 2.0 ** -16).to(torch.int32)     # z < 2^-6: multiples of 2^-9
     code = torch.where(z < 2.0 ** -6, tiny, normal).clamp(max=0x7E)
     if at_least_one:
-        code = torch.where((z > 0) & (code == 0), 1, code)
+        code = torch.where((x > 0) & (scale[:, None] > 0) & (code == 0), 1, code)
     code = code | torch.where((x < 0) & (code > 0), 0x80, 0)
     return code.to(torch.uint8).view(-1).view(torch.float8_e4m3fn), scale
 
@@ -317,7 +317,7 @@ def _plain_adamw(s):
     s["step"] += 1
     t = s["step"]
     norm = s["grads"].double().square().sum().sqrt().float()     # summed in 64 bits, as the operator is defined
-    factor = torch.where(norm > s["max_norm"], s["max_norm"] / norm, 1.0)
+    factor = torch.where(norm > s["max_norm"], torch.full_like(norm, s["max_norm"]) / norm, 1.0)
     size, root = _LR / (1 - _BETA1 ** t), 1 / math.sqrt(1 - _BETA2 ** t)
     first = 0
     for i, (p, grad, decay) in enumerate(zip(s["param_list"], s["grad_list"], s["decays"])):
