@@ -271,7 +271,7 @@ int echo_stats(echo_ctx *ctx, echo_stats_t *out);
 int echo_step_times(echo_ctx *ctx, float *out_ms, int32_t cap);
 
 /* Message for the last error on this context (ctx-owned, valid until the next call); "" if none.
- * With ctx == NULL: the message of the last failed echo_init on this thread. */
+ * With ctx == NULL: the message of the last failed echo_init on this thread, or of its last refused call of echo_learner.h. */
 const char *echo_last_error(const echo_ctx *ctx);
 
 void echo_destroy(echo_ctx *ctx);

@@ -1,0 +1,132 @@
+/*
+ * echo_learner.h -- the learner's step on one MI355X: what turns a scored batch of rollouts into the next snapshot.
+ *
+ * The rollout side (echo.h) hands over tokens with the probability under which each was drawn; the learner scores the
+ * same tokens under its own weights, forms the paper's clipped objective from the ratios (App. "GRPO-Style Policy
+ * Gradient Objective"), and updates the weights whose bf16 form is the next snapshot (echo_load_policy).  The
+ * operators here work on the learner's own tensors in device memory and need no context.
+ *
+ * Conventions: as in echo.h, functions return 0 or a negative echo_status and never throw, abort or print;
+ * echo_last_error(NULL) has the message of the calling thread's last refused call.  Device pointers live on the GPU that
+ * `stream` (a hipStream_t; NULL: the null stream of the current device) belongs to, and are aligned to their elements; no further
+ * alignment is needed.  Calls queue their kernels on `stream` and return without waiting; host arrays may be freed then.
+ * The caller owns every buffer: nothing is allocated, nothing is kept from one call to the next.  A workspace has the
+ * bytes that its size function gives (256-byte aligned), starts from any contents and must not be shared by calls that
+ * can overlap in time.  Calls can be recorded into a HIP graph.  Results do not depend on anything but the arguments: the
+ * same call gives the same bits.
+ */
+#ifndef ECHO_LEARNER_H_
+#define ECHO_LEARNER_H_
+
+#include "echo.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Element types beyond ECHO_F32 and ECHO_BF16: IEEE half precision, and the 8-bit float of 4 exponent and 3 significand
+ * bits without infinities (OCP 8-bit floating point, E4M3). */
+enum { ECHO_F16 = 2, ECHO_E4M3 = 3 };
+
+/* Rows of logits.  Row t starts at element t * row_stride.  Its distribution is softmax(logits / temperature); an entry of
+ * -inf is ruled out; a row of nothing else has log-sum -inf, log-probabilities -inf, entropy 0 and gradient 0; a row that holds a
+ * NaN or +inf gives NaN.  A row whose target lies outside 0 .. vocab - 1 (say -1) takes no part: its logits are not read and its
+ * outputs are 0 (top ids -1). */
+typedef struct {
+  const void *logits;      /* device [rows, row_stride] */
+  const int32_t *targets;  /* device [rows]: the given token of each row */
+  int64_t rows, row_stride; /* row_stride >= vocab */
+  int32_t vocab;
+  int32_t dtype;           /* ECHO_F32, ECHO_BF16 or ECHO_F16 */
+  float temperature;       /* > 0, 1 / temperature finite */
+} echo_logits;
+
+/* Log-probability of the given token, entropy, log-sum and the top_k most probable entries of every row:
+ *   lse = ln sum_j exp(x_j / T)      logprobs = x_target / T - lse      entropy = -sum_j p_j ln p_j
+ *   top_ids / top_logprobs [rows, top_k]: entries by descending logit, of equal ones the lowest index first; entries of -inf are no
+ *   alternatives: where fewer are left the rest is id -1, log-probability -inf.
+ * out_* device f32 / int32, each nullable; top_k 0 .. min(ECHO_TOP_MAX, vocab), both top outputs or neither as top_k says.
+ * targets may be NULL: every row takes part, out_logprobs must be NULL.  In rows with NaN the ids are of entries of the row, which
+ * ones is not said. */
+#define ECHO_TOP_MAX 64
+size_t echo_token_logprobs_workspace(const echo_logits *x, int32_t top_k);
+int echo_token_logprobs(const echo_logits *x, int32_t top_k, float *out_logprobs, float *out_entropy, float *out_lse, int32_t *out_top_ids,
+                        float *out_top_logprobs, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradient of sum_t grad_logprobs[t] logprobs[t] + grad_entropy[t] entropy[t] with respect to the logits:
+ *   out[t][j] = (grad_logprobs (1[j = target] - p_j) - grad_entropy p_j (ln p_j + entropy)) / T,   p_j = exp(x_j / T - lse)
+ * lse and entropy device f32 [rows], as echo_token_logprobs gave them.  grad_entropy may be NULL (the entropy is not read then), and so may
+ * grad_logprobs, but not both; without targets every row takes part and grad_logprobs must be NULL.  out: device, the logits' type, rows out_stride elements apart; may be the logits themselves (same stride).  Every row is
+ * written, one that takes no part with 0. */
+int echo_token_logprobs_grad(const echo_logits *x, const float *lse, const float *entropy, const float *grad_logprobs, const float *grad_entropy,
+                             void *out, int64_t out_stride, void *stream);
+
+/* The objective's coefficients.  ratio = exp(logprob - old_logprob). */
+typedef struct {
+  float clip_low, clip_high; /* the clipped ratio lies in [1 - clip_low, 1 + clip_high]; >= 0 */
+  float ratio_cap;           /* > 0, may be infinite: the free ratio counts as at most this (bounds the loss where the advantage is negative) */
+  float sampler_cap;         /* > 0, may be infinite: bound C of the truncated importance weight min(exp(old - sampler), C) */
+  float kl_coef;             /* weight of the divergence from the reference policy */
+  float entropy_coef;        /* weight of the entropy bonus */
+} echo_policy_loss_opts;
+
+/* Loss of every token and its gradient with respect to the logits, in one call:
+ *   S    = min( min(ratio, ratio_cap) A, clip(ratio, 1 - clip_low, 1 + clip_high) A )
+ *   loss = weight ( -min(exp(old - sampler), C) S + kl_coef (exp(ref - lp) - (ref - lp) - 1) - entropy_coef entropy ),   lp the log-probability
+ *   out_grad[t][j] = d loss[t] / d x_j; the importance weight is held constant, and of the two terms of S the first counts where they
+ *   are equal.
+ * advantages, old_logprobs: device f32 [rows]; weights (NULL: 1), sampler_logprobs (NULL: importance weight 1), ref_logprobs (needed if
+ * kl_coef is not 0): device f32 [rows].  A row of weight 0 takes no part, as one without a target.  out_loss, out_logprobs, out_entropy:
+ * device f32 [rows], nullable; out_grad as in echo_token_logprobs_grad (nullable: the loss alone). */
+size_t echo_policy_loss_workspace(const echo_logits *x);
+int echo_policy_loss(const echo_logits *x, const float *advantages, const float *old_logprobs, const float *weights, const float *sampler_logprobs,
+                     const float *ref_logprobs, const echo_policy_loss_opts *opts, float *out_loss, float *out_logprobs, float *out_entropy, void *out_grad,
+                     int64_t grad_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Euclidean norm of n_tensors gradients taken together, summed in f64, rounded to f32 once: *out_norm (device).
+ * grads host array of device pointers, numel host [n_tensors] (0 allowed), dtype ECHO_F32, ECHO_BF16 or ECHO_F16. */
+size_t echo_grad_norm_workspace(const int64_t *numel, int32_t n_tensors);
+int echo_grad_norm(const void *const *grads, const int64_t *numel, int32_t n_tensors, int32_t dtype, float *out_norm, void *workspace,
+                   size_t workspace_bytes, void *stream);
+
+/* One AdamW step over many tensors.  With g the gradient, scaled by max_norm / norm where norm exceeds max_norm:
+ *   m = beta1 m + (1 - beta1) g        v = beta2 v + ((1 - beta2) g) g
+ *   p = p (1 - lr weight_decay) - (m / (sqrt(v) / sqrt(1 - beta2^step) + eps)) lr / (1 - beta1^step)
+ * Constants are formed in f64 and rounded to f32 once; every operation on elements is one f32 operation in the order written, so results are
+ * the same bits on every run.  If the norm is given and not finite, nothing is written.
+ *
+ * m and v hold tensor after tensor, each from a multiple of ECHO_ADAMW_BLOCK elements on (echo_adamw_state_numel elements in all).
+ * state_dtype ECHO_F32: f32, 8 bytes an element for both.  ECHO_E4M3: 2 bytes.  Every ECHO_ADAMW_BLOCK consecutive elements share a scale,
+ * the largest magnitude among them / 448 (0 below 2^-100: all codes are 0 then), and an element is code * scale, rounded to one of the two nearest
+ * codes with a probability by its distance to each: an average that moves by a thousandth per step would otherwise stand still at three
+ * significand bits.  A positive v keeps a positive code, so no denominator vanishes.
+ * param_dtype ECHO_F32: p is the master copy; snapshot (nullable) receives its bf16 values (to nearest even), laid out as the caller's
+ * pointers say, for instance in the order of echo_load_policy's blob.  ECHO_BF16: p is held in bf16, rounded by chance likewise; snapshot must be NULL.
+ * The random bits of element i of the states' numbering are those of Philox-4x32-10 with counter (i / 4, step, purpose) and key seed, word i mod 4:
+ * purpose 0, low half m, high half v; purpose 1, low half p.
+ * Without a norm, a gradient that is not finite goes through the formulas; an 8-bit block with an infinite element becomes NaN.
+ * No two tensors of a call may overlap. */
+#define ECHO_ADAMW_BLOCK 256
+typedef struct {
+  void *const *params;         /* host [n_tensors] of device pointers */
+  const void *const *grads;    /* host [n_tensors] of device pointers */
+  void *const *snapshot;       /* host [n_tensors] of device pointers, or NULL */
+  const int64_t *numel;        /* host [n_tensors], 0 allowed */
+  const double *weight_decay;  /* host [n_tensors] */
+  void *m, *v;                 /* device */
+  float *m_scale, *v_scale;    /* device [state_numel / ECHO_ADAMW_BLOCK], ECHO_E4M3 only (NULL otherwise) */
+  const float *norm;           /* device: *norm, or NULL: no clipping */
+  double lr, beta1, beta2, eps; /* lr >= 0, 0 <= beta < 1, eps > 0 */
+  int64_t step;                /* 1 for the first step, at most 2^31 - 1 */
+  uint64_t seed;
+  float max_norm;              /* > 0, may be infinite */
+  int32_t n_tensors;
+  int32_t param_dtype, grad_dtype, state_dtype; /* grad_dtype: ECHO_F32 or ECHO_BF16 */
+} echo_adamw_args;
+int64_t echo_adamw_state_numel(const int64_t *numel, int32_t n_tensors); /* -1 on invalid arguments */
+int echo_adamw_step(const echo_adamw_args *args, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* ECHO_LEARNER_H_ */

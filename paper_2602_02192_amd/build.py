@@ -30,7 +30,7 @@ def _stale(obj, src):
         return True
     t = os.path.getmtime(obj)
     deps = [src] + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
-    deps.append(os.path.join(HERE, "..", "include", "echo.h"))
+    deps += [os.path.join(HERE, "..", "include", f) for f in ("echo.h", "echo_learner.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -4,6 +4,9 @@
 
 int echo_static_scratch_resolve(int device);   // echo_noalloc.hip: looks up this GPU's copy of the library's static scratch
 
+// The message of a refused call that has no context (echo_learner.hip).
+void echo_set_call_error(const char *msg) { g_init_error = msg; }
+
 // =================================================================================================== C ABI
 extern "C" {
 

@@ -1,0 +1,331 @@
+"""The learner's operators (include/echo_learner.h) on torch tensors: log-probabilities of given tokens with entropy and top
+alternatives, the policy loss with its gradient, the norm of many gradients and the AdamW step that ends in a snapshot.
+
+Argument marshalling only: the arithmetic is in the library's HIP kernels.  Calls are queued on the current stream of the
+tensors' GPU and do not wait; the usual rules of torch for tensors that other streams use apply to them.  Arguments that the library
+refuses raise echo.EchoError, tensors that it could not be handed (another type, device or layout) ValueError."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import NamedTuple, Optional, Sequence
+
+import numpy as np
+import torch
+
+from .echo import ECHO_BF16, ECHO_F32, EchoError, lib
+
+ECHO_F16, ECHO_E4M3 = 2, 3
+BLOCK = 256      # elements of the states that share a scale; every tensor's states start at a multiple of it
+TOP_MAX = 64
+
+EXPORTS = ["echo_token_logprobs_workspace", "echo_token_logprobs", "echo_token_logprobs_grad", "echo_policy_loss_workspace", "echo_policy_loss",
+           "echo_grad_norm_workspace", "echo_grad_norm", "echo_adamw_state_numel", "echo_adamw_step"]
+
+
+class _Logits(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("targets", C.c_void_p), ("rows", C.c_int64), ("row_stride", C.c_int64), ("vocab", C.c_int32), ("dtype", C.c_int32),
+                ("temperature", C.c_float)]
+
+
+class _LossOpts(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("clip_low", "clip_high", "ratio_cap", "sampler_cap", "kl_coef", "entropy_coef")]
+
+
+class _AdamW(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("params", "grads", "snapshot", "numel", "weight_decay", "m", "v", "m_scale", "v_scale", "norm")] + \
+               [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps")] + [("step", C.c_int64), ("seed", C.c_uint64), ("max_norm", C.c_float)] + \
+               [(n, C.c_int32) for n in ("n_tensors", "param_dtype", "grad_dtype", "state_dtype")]
+
+
+_P = C.c_void_p
+lib.echo_token_logprobs_workspace.restype = C.c_size_t
+lib.echo_token_logprobs_workspace.argtypes = [C.POINTER(_Logits), C.c_int32]
+lib.echo_token_logprobs.argtypes = [C.POINTER(_Logits), C.c_int32, _P, _P, _P, _P, _P, _P, C.c_size_t, _P]
+lib.echo_token_logprobs_grad.argtypes = [C.POINTER(_Logits), _P, _P, _P, _P, _P, C.c_int64, _P]
+lib.echo_policy_loss_workspace.restype = C.c_size_t
+lib.echo_policy_loss_workspace.argtypes = [C.POINTER(_Logits)]
+lib.echo_policy_loss.argtypes = [C.POINTER(_Logits), _P, _P, _P, _P, _P, C.POINTER(_LossOpts), _P, _P, _P, _P, C.c_int64, _P, C.c_size_t, _P]
+lib.echo_grad_norm_workspace.restype = C.c_size_t
+lib.echo_grad_norm_workspace.argtypes = [_P, C.c_int32]
+lib.echo_grad_norm.argtypes = [_P, _P, C.c_int32, C.c_int32, _P, _P, C.c_size_t, _P]
+lib.echo_adamw_state_numel.restype = C.c_int64
+lib.echo_adamw_state_numel.argtypes = [_P, C.c_int32]
+lib.echo_adamw_step.argtypes = [C.POINTER(_AdamW), _P]
+
+_DTYPE = {torch.float32: ECHO_F32, torch.bfloat16: ECHO_BF16, torch.float16: ECHO_F16, torch.float8_e4m3fn: ECHO_E4M3}
+
+
+def _chk(rc: int) -> None:
+    if rc != 0:
+        raise EchoError(rc, lib.echo_last_error(None).decode())
+
+
+class _on:
+    """The stream of a call on `device`, with that device current."""
+
+    def __init__(self, device: torch.device):
+        if device.type != "cuda":
+            raise ValueError(f"tensors must live on a GPU, got {device}")
+        self.index = device.index
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.before != self.index:
+            torch.cuda.set_device(self.index)
+        return torch.cuda.current_stream(self.index).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            torch.cuda.set_device(self.before)
+
+
+def _vector(t: Optional[torch.Tensor], name: str, rows: int, like: torch.Tensor, dtype=torch.float32):
+    """Address of a contiguous [rows] tensor next to `like`; None stays None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != rows or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {rows} on {like.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _matrix(t: torch.Tensor, name: str):
+    """Row stride of a two-dimensional tensor whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must have two dimensions and contiguous rows, got shape {tuple(t.shape)}, strides {t.stride()}")
+    if t.shape[0] <= 1:
+        return max(t.shape[1], 1)
+    if t.stride(0) < t.shape[1]:
+        raise ValueError(f"the rows of {name} overlap: stride {t.stride(0)} for {t.shape[1]} entries")
+    return t.stride(0)
+
+
+def _logits(x: torch.Tensor, targets, temperature: float) -> _Logits:
+    if x.dtype not in (torch.float32, torch.bfloat16, torch.float16):
+        raise ValueError(f"logits must be float32, bfloat16 or float16, got {x.dtype}")
+    stride = _matrix(x, "logits")
+    return _Logits(x.data_ptr(), _vector(targets, "targets", x.shape[0], x, torch.int32), x.shape[0], stride, x.shape[1], _DTYPE[x.dtype], temperature)
+
+
+def _workspace(nbytes: int, like: torch.Tensor):
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+
+
+def _addr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+# ---- log-probabilities ----------------------------------------------------------------------------------------------------
+
+class TokenLogprobs(NamedTuple):
+    """f32 [rows], None where there are no targets; f32 [rows] twice; int32 and f32 [rows, top_k], None where top_k is 0."""
+    logprobs: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_ids: Optional[torch.Tensor]
+    top_logprobs: Optional[torch.Tensor]
+
+
+def _token_logprobs(logits, targets, temperature, top_k) -> TokenLogprobs:
+    x = _logits(logits, targets, temperature)
+    rows, dev = logits.shape[0], logits.device
+    with _on(dev) as stream:
+        f = torch.empty(3 if targets is not None else 2, rows, dtype=torch.float32, device=dev)
+        ids = torch.empty(rows, top_k, dtype=torch.int32, device=dev) if top_k > 0 else None
+        tops = torch.empty(rows, top_k, dtype=torch.float32, device=dev) if top_k > 0 else None
+        need = lib.echo_token_logprobs_workspace(C.byref(x), top_k)
+        ws = _workspace(need, logits)
+        entropy, lse = f[0], f[1]
+        logprobs = f[2] if targets is not None else None
+        _chk(lib.echo_token_logprobs(C.byref(x), top_k, _addr(logprobs), entropy.data_ptr(), lse.data_ptr(), _addr(ids), _addr(tops), _addr(ws), need, stream))
+    return TokenLogprobs(logprobs, entropy, lse, ids, tops)
+
+
+class _Differentiable(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, temperature, top_k):
+        r = _token_logprobs(logits, targets, temperature, top_k)
+        ctx.save_for_backward(logits, targets, r.lse, r.entropy)
+        ctx.temperature = temperature
+        ctx.mark_non_differentiable(*(t for t in (r.lse, r.top_ids, r.top_logprobs) if t is not None))
+        ctx.set_materialize_grads(False)
+        return tuple(r)
+
+    @staticmethod
+    def backward(ctx, g, h, *_):
+        logits, targets, lse, entropy = ctx.saved_tensors
+        if g is None and h is None:
+            return None, None, None, None
+        g, h = (None if t is None else t.contiguous() for t in (g, h))
+        return token_logprobs_grad(logits, targets, lse, entropy, g, h, temperature=ctx.temperature), None, None, None
+
+
+def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, *, temperature: float = 1.0, top_k: int = 0) -> TokenLogprobs:
+    """Log-probability of the given token, entropy, log-sum and the top_k most probable entries of every row of `logits` [rows, vocab]
+    (float32, bfloat16 or float16; rows may lie further apart than vocab).  `targets` int32 [rows]: a row whose target lies outside the
+    vocabulary takes no part (zeros, ids -1); without targets every row does.  logprobs and entropy can be differentiated with respect to the
+    logits."""
+    if logits.requires_grad and torch.is_grad_enabled():
+        return TokenLogprobs(*_Differentiable.apply(logits, targets, temperature, top_k))
+    return _token_logprobs(logits, targets, temperature, top_k)
+
+
+def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor], lse: torch.Tensor, entropy: Optional[torch.Tensor], grad_logprobs: Optional[torch.Tensor],
+                        grad_entropy: Optional[torch.Tensor] = None, *, temperature: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of sum(grad_logprobs * logprobs + grad_entropy * entropy) with respect to the logits, from what token_logprobs returned.
+    `out` may be the logits themselves."""
+    x = _logits(logits, targets, temperature)
+    rows = logits.shape[0]
+    a = [_vector(t, n, rows, logits) for t, n in ((lse, "lse"), (entropy, "entropy"), (grad_logprobs, "grad_logprobs"), (grad_entropy, "grad_entropy"))]
+    with _on(logits.device) as stream:
+        out = _grad_like(logits, out)
+        _chk(lib.echo_token_logprobs_grad(C.byref(x), *a, out.data_ptr(), _matrix(out, "out"), stream))
+    return out
+
+
+def _grad_like(logits, out):
+    if out is None:
+        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    if out.dtype != logits.dtype or out.shape != logits.shape or out.device != logits.device:
+        raise ValueError("the gradient must have the logits' type, shape and device")
+    return out
+
+
+# ---- the policy loss --------------------------------------------------------------------------------------------------------
+
+class PolicyLoss(NamedTuple):
+    """f32 [rows] each; the gradient of the summed loss in the logits' type and shape, None where it was not asked for."""
+    loss: torch.Tensor
+    logprobs: torch.Tensor
+    entropy: torch.Tensor
+    grad_logits: Optional[torch.Tensor]
+
+
+def policy_loss(logits: torch.Tensor, targets: torch.Tensor, advantages: torch.Tensor, old_logprobs: torch.Tensor, *, weights: Optional[torch.Tensor] = None,
+                sampler_logprobs: Optional[torch.Tensor] = None, ref_logprobs: Optional[torch.Tensor] = None, temperature: float = 1.0, clip_low: float = 0.2,
+                clip_high: float = 0.2, ratio_cap: float = 4.0, sampler_cap: float = float("inf"), kl_coef: float = 0.0, entropy_coef: float = 0.0,
+                want_grad: bool = True, grad_out: Optional[torch.Tensor] = None) -> PolicyLoss:
+    """The paper's clipped objective token by token, and d sum(loss) / d logits: `logits.backward(result.grad_logits)` carries it on into
+    the network.  `weights` [rows] scale the tokens (1 / tokens of the batch for a mean); a token of weight 0 takes no part.
+    `grad_out` may be the logits themselves."""
+    x = _logits(logits, targets, temperature)
+    rows, dev = logits.shape[0], logits.device
+    a = [_vector(t, n, rows, logits) for t, n in ((advantages, "advantages"), (old_logprobs, "old_logprobs"), (weights, "weights"),
+                                                  (sampler_logprobs, "sampler_logprobs"), (ref_logprobs, "ref_logprobs"))]
+    o = _LossOpts(clip_low, clip_high, ratio_cap, sampler_cap, kl_coef, entropy_coef)
+    with _on(dev) as stream:
+        f = torch.empty(3, rows, dtype=torch.float32, device=dev)
+        grad = _grad_like(logits, grad_out) if want_grad or grad_out is not None else None
+        need = lib.echo_policy_loss_workspace(C.byref(x))
+        ws = _workspace(need, logits)
+        loss, logprobs, entropy = f[0], f[1], f[2]
+        _chk(lib.echo_policy_loss(C.byref(x), *a, C.byref(o), loss.data_ptr(), logprobs.data_ptr(), entropy.data_ptr(), _addr(grad),
+                                  0 if grad is None else _matrix(grad, "grad_out"), _addr(ws), need, stream))
+    return PolicyLoss(loss, logprobs, entropy, grad)
+
+
+# ---- the update -----------------------------------------------------------------------------------------------------------------
+
+def _same(tensors: Sequence[torch.Tensor], name: str, dtypes):
+    """(addresses, sizes) of contiguous tensors of one type on one device."""
+    if not tensors:
+        raise ValueError(f"no {name}")
+    dtype, device = tensors[0].dtype, tensors[0].device
+    if dtype not in dtypes:
+        raise ValueError(f"{name} must be of a type among {dtypes}, got {dtype}")
+    for i, t in enumerate(tensors):
+        if t.dtype != dtype or t.device != device or not t.is_contiguous():
+            raise ValueError(f"{name}[{i}] must be contiguous, {dtype} and on {device}")
+    return np.array([t.data_ptr() for t in tensors], np.uint64), np.array([t.numel() for t in tensors], np.int64)
+
+
+def grad_norm(grads: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Euclidean norm of all the gradients together: a float32 tensor of one value on their GPU (`out`, or a new one)."""
+    addresses, numel = _same(grads, "grads", (torch.float32, torch.bfloat16, torch.float16))
+    like = grads[0]
+    with _on(like.device) as stream:
+        if out is None:
+            out = torch.empty((), dtype=torch.float32, device=like.device)
+        elif out.dtype != torch.float32 or out.numel() != 1 or out.device != like.device:
+            raise ValueError("out must be one float32 value on the gradients' device")
+        need = lib.echo_grad_norm_workspace(numel.ctypes.data, len(grads))
+        ws = _workspace(need, like)
+        _chk(lib.echo_grad_norm(addresses.ctypes.data, numel.ctypes.data, len(grads), _DTYPE[like.dtype], out.data_ptr(), _addr(ws), need, stream))
+    return out
+
+
+def state_numel(params: Sequence[torch.Tensor]) -> int:
+    """Elements of m, and of v, for these parameters: each tensor's size rounded up to BLOCK."""
+    return sum(-(-p.numel() // BLOCK) * BLOCK for p in params)
+
+
+def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: torch.Tensor, v: torch.Tensor, *, step: int, lr: float, beta1: float = 0.9,
+               beta2: float = 0.999, eps: float = 1e-8, weight_decay=0.0, m_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+               snapshot: Optional[Sequence[torch.Tensor]] = None, norm: Optional[torch.Tensor] = None, max_norm: float = float("inf"), seed: int = 0) -> None:
+    """One AdamW step in place.  `params` all float32 or all bfloat16, `grads` all float32 or all bfloat16, of equal sizes.  `m` and `v`: flat
+    tensors of state_numel(params) elements, float32, or float8_e4m3fn with float32 scales (one per BLOCK elements).  `weight_decay`: one
+    number, or one per tensor.  `snapshot`: bfloat16 tensors that receive the new values of float32 parameters.  `norm` (from grad_norm):
+    gradients are scaled to at most `max_norm`, and a norm that is not finite leaves everything as it is.  `seed` and `step` choose the random
+    bits by which 8-bit states and bfloat16 parameters are rounded."""
+    pa, numel = _same(params, "params", (torch.float32, torch.bfloat16))
+    ga, gn = _same(grads, "grads", (torch.float32, torch.bfloat16))
+    like, dev = params[0], params[0].device
+    if not np.array_equal(gn, numel) or grads[0].device != dev:
+        raise ValueError("grads must match params in number, sizes and device")
+    sa = None
+    if snapshot is not None:
+        sa, sn = _same(snapshot, "snapshot", (torch.bfloat16,))
+        if not np.array_equal(sn, numel) or snapshot[0].device != dev:
+            raise ValueError("snapshot must match params in number, sizes and device")
+    n = int((-(-numel // BLOCK)).sum()) * BLOCK
+    if m.dtype not in (torch.float32, torch.float8_e4m3fn):
+        raise ValueError(f"m and v must be float32 or float8_e4m3fn, got {m.dtype}")
+    ma, va = _vector(m, "m", n, like, m.dtype), _vector(v, "v", n, like, m.dtype)
+    msa, vsa = _vector(m_scale, "m_scale", n // BLOCK, like), _vector(v_scale, "v_scale", n // BLOCK, like)
+    if norm is not None and (norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != dev):
+        raise ValueError("norm must be one float32 value on the parameters' device")
+    decay = np.full(len(params), weight_decay, np.float64) if isinstance(weight_decay, (int, float)) else np.array(weight_decay, np.float64)
+    if decay.shape != (len(params),):
+        raise ValueError(f"weight_decay must be one number or {len(params)}")
+    a = _AdamW(pa.ctypes.data, ga.ctypes.data, None if sa is None else sa.ctypes.data, numel.ctypes.data, decay.ctypes.data, ma, va, msa, vsa, _addr(norm),
+               lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, max_norm, len(params), _DTYPE[like.dtype], _DTYPE[grads[0].dtype], _DTYPE[m.dtype])
+    with _on(dev) as stream:
+        _chk(lib.echo_adamw_step(C.byref(a), stream))
+
+
+class AdamW:
+    """The state of adamw_step for a list of parameters.  `step(grads)` takes the gradients given, or each parameter's .grad, and
+    returns their norm where `max_norm` is finite (a step whose norm is not finite changes nothing but the count)."""
+
+    def __init__(self, params: Sequence[torch.Tensor], lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0, *, max_norm: float = float("inf"),
+                 state_dtype: torch.dtype = torch.float32, snapshot: Optional[Sequence[torch.Tensor]] = None, seed: int = 0):
+        if state_dtype not in (torch.float32, torch.float8_e4m3fn):
+            raise ValueError(f"states must be float32 or float8_e4m3fn, got {state_dtype}")
+        self.params, self.snapshot = list(params), None if snapshot is None else list(snapshot)
+        self.lr, self.betas, self.eps, self.weight_decay, self.max_norm, self.seed, self.steps = lr, betas, eps, weight_decay, max_norm, seed, 0
+        n, dev = state_numel(self.params), self.params[0].device
+        self.m, self.v = (torch.zeros(n, dtype=torch.uint8 if state_dtype != torch.float32 else torch.float32, device=dev).view(state_dtype) for _ in range(2))
+        self.m_scale, self.v_scale = (torch.zeros(n // BLOCK, device=dev) for _ in range(2)) if state_dtype != torch.float32 else (None, None)
+
+    def step(self, grads: Optional[Sequence[torch.Tensor]] = None) -> Optional[torch.Tensor]:
+        params = [p.detach() for p in self.params]
+        grads = [p.grad for p in self.params] if grads is None else list(grads)
+        if any(g is None for g in grads):
+            raise ValueError("a parameter has no gradient")
+        norm = grad_norm(grads) if self.max_norm != float("inf") else None
+        adamw_step(params, grads, self.m, self.v, step=self.steps + 1, lr=self.lr, beta1=self.betas[0], beta2=self.betas[1], eps=self.eps,
+                   weight_decay=self.weight_decay, m_scale=self.m_scale, v_scale=self.v_scale, snapshot=self.snapshot, norm=norm, max_norm=self.max_norm,
+                   seed=self.seed)
+        self.steps += 1
+        return norm
+
+    def state_dict(self) -> dict:
+        return dict(m=self.m, v=self.v, m_scale=self.m_scale, v_scale=self.v_scale, steps=self.steps, seed=self.seed)
+
+    def load_state_dict(self, state: dict) -> None:
+        for k in ("m", "v", "m_scale", "v_scale"):
+            mine, theirs = getattr(self, k), state[k]
+            if (mine is None) != (theirs is None) or (mine is not None and (mine.shape != theirs.shape or mine.dtype != theirs.dtype)):
+                raise ValueError(f"{k} does not fit these parameters")
+            if mine is not None:
+                mine.copy_(theirs)
+        self.steps, self.seed = int(state["steps"]), int(state["seed"])
