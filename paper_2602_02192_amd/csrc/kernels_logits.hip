@@ -41,6 +41,8 @@ template <int DT> __device__ __forceinline__ vec16 pack(const float *v) {
   }
   return q;
 }
+// The compiler would keep the widened elements of a vector from one use to the next, in twice its registers; after this it widens them again.
+__device__ __forceinline__ void as_loaded(vec16 &q) { asm volatile("" : "+v"(q)); }
 template <int DT> __device__ __forceinline__ vec16 filled(float f) {
   float v[8] = {f, f, f, f, f, f, f, f};
   return pack<DT>(v);
@@ -138,29 +140,31 @@ template <int DT, int N> __device__ __forceinline__ float largest(const vec16 *q
   }
   return top;
 }
-template <int DT, int N> __device__ __forceinline__ void add_entries(RowStats &s, const vec16 *q, float top, float c) {
+template <int DT, int N> __device__ __forceinline__ void add_entries(RowStats &s, vec16 *q, float top, float c) {
   s = moved(s, top, c);
   const float from = top == -INFINITY ? 0.f : top;
 #pragma unroll
-  for (int u = 0; u < N; ++u)
+  for (int u = 0; u < N; ++u) {
+    as_loaded(q[u]);
 #pragma unroll
     for (int e = 0; e < Elem<DT>::VEC; ++e) {
       const float d = (element<DT>(q[u], e) - from) * c, p = __builtin_amdgcn_exp2f(d);
       s.sum += p;
       s.turn = fmaf(p, fmaxf(d, -200.f), s.turn);
     }
+  }
 }
 
 // A part of a row: its statistics, and the given entry's logit where it holds it.
 struct RowPart { RowStats s; float given; };
 struct Parts { RowPart *part; uint64_t *top; };   // [rows, splits], [rows, splits, top_k]
 
-// The k largest of n <= CANDIDATES different keys, in order, by their rank among all; the rest of out is 0.
+// The k largest of n <= CANDIDATES keys (different ones but for 0), in order, by their rank among all; what is left of out is 0.
 __device__ __forceinline__ void select_top(const uint64_t *keys, int n, int k, uint64_t *out) {
   for (int i = threadIdx.x; i < n; i += THREADS) {
     const uint64_t mine = keys[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += keys[j] > mine;
+    for (int j = 0; j < n; ++j) rank += keys[j] > mine || (keys[j] == mine && j < i);
     if (rank < k) out[rank] = mine;
   }
   for (int i = n + threadIdx.x; i < k; i += THREADS) out[i] = 0;
@@ -213,6 +217,7 @@ template <int DT, bool TOP> __global__ __launch_bounds__(THREADS) void stats_ker
 #pragma unroll
     for (int u = 0; u < BATCH; ++u) {
       if (!(of_vector[u] >= floor)) continue;
+      as_loaded(q[u]);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         const float v = element<DT>(q[u], e);
@@ -229,13 +234,15 @@ template <int DT, bool TOP> __global__ __launch_bounds__(THREADS) void stats_ker
     for (int k = 0; k < top_k; ++k) {
       uint64_t best = 0;
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u)
+      for (int u = 0; u < BATCH; ++u) {
+        as_loaded(q[u]);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
           const float v = element<DT>(q[u], e);
           const uint64_t key = order_key(v, begin + (u * THREADS + (int)threadIdx.x) * VEC + e);
           if (v >= floor && key < last && key > best) best = key;
         }
+      }
       for (int o = 32; o > 0; o >>= 1) { const uint64_t b = __shfl_xor(best, o, 64); best = b > best ? b : best; }
       __syncthreads();
       if (threadIdx.x % 64 == 0) keys[threadIdx.x / 64] = best;
@@ -278,16 +285,30 @@ template <bool TOP> __global__ __launch_bounds__(THREADS) void stats_finish_kern
     }
   }
   if constexpr (TOP) {
-    __shared__ uint64_t best[ECHO_TOP_MAX];
-    const int k = out.top_k, n = splits * k;
-    const uint64_t *keys = p.top + t * n;
-    if (live)
-      for (int i = threadIdx.x; i < n; i += THREADS) {
-        const uint64_t mine = keys[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += keys[j] > mine || (keys[j] == mine && j < i);   // (only empty places are equal)
-        if (rank < k) best[rank] = mine;
+    // The parts' lists, as many at a time as fit: of the best so far and of the new ones only those count that reach the last of a list, since that many
+    // entries are as large as it is.
+    __shared__ uint64_t keys[CANDIDATES], best[ECHO_TOP_MAX], bound;
+    __shared__ uint32_t count;
+    const int k = out.top_k, n = splits * k, at_once = (CANDIDATES / k - 1) * k;
+    const uint64_t *lists = p.top + t * n;
+    if (threadIdx.x == 0) { bound = 1; count = 0; }
+    __syncthreads();
+    for (int done = 0; live && done < n; done += at_once) {
+      const int more = min(n - done, at_once);
+      for (int i = threadIdx.x; i < more / k; i += THREADS) atomicMax((unsigned long long *)&bound, lists[done + i * k + k - 1]);
+      __syncthreads();
+      const uint64_t least = bound;
+      for (int i = threadIdx.x; i < more; i += THREADS) {
+        const uint64_t key = lists[done + i];
+        if (key >= least) keys[atomicAdd(&count, 1u)] = key;
       }
+      if (done && threadIdx.x < k && best[threadIdx.x] >= least) keys[atomicAdd(&count, 1u)] = best[threadIdx.x];
+      __syncthreads();
+      select_top(keys, count, k, best);
+      __syncthreads();
+      if (threadIdx.x == 0) { bound = max(best[k - 1], (uint64_t)1); count = 0; }
+      __syncthreads();
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < k; i += THREADS) {
       const uint64_t key = live ? best[i] : 0;
@@ -405,6 +426,54 @@ template <int DT, bool LOSS> __global__ __launch_bounds__(THREADS) void grad_ker
   }
 }
 
+// A whole row by one workgroup: its first N vectors a thread stay in registers between the statistics and the gradient, what is beyond them is read
+// again.
+template <int DT, int W, int N> __global__ __launch_bounds__(W) void loss_row_kernel(LogitRows r, PolicyTerms terms, LossOutputs out) {
+  constexpr int VEC = Elem<DT>::VEC, AGAIN = 4;
+  __shared__ RowStats sh[W / 64];
+  const int64_t t = blockIdx.x;
+  const auto *x = (const typename Elem<DT>::type *)r.x + t * r.stride;
+  auto *o = (typename Elem<DT>::type *)out.grad + t * out.stride;
+  const int mine = threadIdx.x * VEC;
+  if (!token_live(r, terms, t)) {
+    if (threadIdx.x == 0) no_loss(out, t);
+    for (int j = mine; j < r.vocab; j += W * VEC) store_vector<DT>(o, j, r.vocab, vec16{0, 0, 0, 0});
+    return;
+  }
+  const float c = LOG2E / r.temperature;
+  const int target = r.targets[t];
+  const float given = widen<DT>(x[target]);
+  vec16 q[N];
+#pragma unroll
+  for (int u = 0; u < N; ++u) q[u] = load_vector<DT>(x, mine + u * W * VEC, r.vocab);
+  RowStats s = {-INFINITY, 0.f, 0.f};
+  for (int j = N * W * VEC; j < r.vocab; j += AGAIN * W * VEC) {
+    vec16 a[AGAIN];
+#pragma unroll
+    for (int u = 0; u < AGAIN; ++u) a[u] = load_vector<DT>(x, j + mine + u * W * VEC, r.vocab);
+    add_entries<DT, AGAIN>(s, a, fmaxf(s.top, largest<DT, AGAIN>(a)), c);
+  }
+  add_entries<DT, N>(s, q, fmaxf(s.top, largest<DT, N>(q)), c);
+  s = block_stats<W / 64>(s, c, sh);   // (its barrier: the target's logit has been read before any gradient is written)
+  const RowGrad g = finish_loss(r, terms, out, t, s, given, threadIdx.x == 0);
+  for (int j = N * W * VEC; j < r.vocab; j += AGAIN * W * VEC) {
+    vec16 a[AGAIN];
+#pragma unroll
+    for (int u = 0; u < AGAIN; ++u) a[u] = load_vector<DT>(x, j + mine + u * W * VEC, r.vocab);
+#pragma unroll
+    for (int u = 0; u < AGAIN; ++u) {
+      const int at = j + mine + u * W * VEC;
+      store_vector<DT>(o, at, r.vocab, grad_vector<DT>(a[u], target - at, g));
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const int at = mine + u * W * VEC;
+    as_loaded(q[u]);
+    store_vector<DT>(o, at, r.vocab, grad_vector<DT>(q[u], target - at, g));
+  }
+}
+
 // The loss alone.
 __global__ __launch_bounds__(64) void loss_finish_kernel(LogitRows r, PolicyTerms terms, Parts p, int splits, LossOutputs out) {
   const int64_t t = blockIdx.x;
@@ -469,6 +538,10 @@ void launch_policy_loss(const LogitRows &x, const PolicyTerms &terms, float *los
   const Split s = split_of(x, false);
   const Parts p = {(RowPart *)workspace, nullptr};
   const LossOutputs o = {loss, logprobs, entropy, grad, grad_stride};
+  if (grad && x.rows >= 200) {
+    FOR_DTYPE(x.dtype, (loss_row_kernel<DT, 1024, DT == ECHO_F32 ? 17 : 19><<<dim3((uint32_t)x.rows), 1024, 0, st>>>(x, terms, o)));
+    return;
+  }
   FOR_DTYPE(x.dtype, (stats_kernel<DT, false><<<dim3((uint32_t)(x.rows * s.splits)), THREADS, 0, st>>>(x, p, s.splits, s.span, 0)));
   if (!grad) {
     loss_finish_kernel<<<dim3((uint32_t)x.rows), 64, 0, st>>>(x, terms, p, s.splits, o);
