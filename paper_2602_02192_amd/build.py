@@ -14,6 +14,7 @@ LIB = os.path.join(HERE, "libecho_hip.so")
 CLIENT = os.path.join(HERE, "echo_client")   # the C-ABI client without Python (csrc/echo_client.cpp)
 TESTS = os.path.join(HERE, "..", "tests")
 SWEEP = os.path.join(TESTS, "_build", "swiglu_sweep")   # the program of tests/test_gpu_swiglu_bits.py
+UPDATE_SWEEP = os.path.join(TESTS, "_build", "update_sweep")   # the program of tests/test_gpu_adamw.py
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -66,6 +67,7 @@ def build(force: bool = True) -> str:
 def build_sweep():
     os.makedirs(os.path.dirname(SWEEP), exist_ok=True)
     _hipcc([os.path.join(TESTS, "swiglu_sweep.hip"), "-o", SWEEP])
+    _hipcc([os.path.join(TESTS, "update_sweep.hip"), "-o", UPDATE_SWEEP])
 
 
 if __name__ == "__main__":

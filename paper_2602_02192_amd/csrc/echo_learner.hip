@@ -99,6 +99,15 @@ int64_t chunks_of(const int64_t *numel, int32_t n, int64_t chunk) {
   return c;
 }
 
+// Chunks of a norm, and their size; -1 as above.
+int64_t norm_chunks(const int64_t *numel, int32_t n, int64_t *chunk) {
+  int64_t total = 0;
+  if (chunks_of(numel, n, 65536) < 0) return -1;
+  for (int i = 0; i < n; ++i) total += numel[i];
+  *chunk = norm_chunk(total);
+  return chunks_of(numel, n, *chunk);
+}
+
 }  // namespace
 
 extern "C" {
@@ -170,7 +179,8 @@ int echo_policy_loss(const echo_logits *x, const float *advantages, const float 
 }
 
 size_t echo_grad_norm_workspace(const int64_t *numel, int32_t n_tensors) {
-  const int64_t c = chunks_of(numel, n_tensors, NORM_CHUNK);
+  int64_t chunk;
+  const int64_t c = norm_chunks(numel, n_tensors, &chunk);
   return c < 0 ? 0 : (size_t)(c + 1) * sizeof(double);
 }
 
@@ -179,7 +189,8 @@ int echo_grad_norm(const void *const *grads, const int64_t *numel, int32_t n_ten
   return guarded([&] {
     const size_t e = element_bytes(dtype);
     if (!e) return refuse(ECHO_EINVAL, "gradients must be ECHO_F32, ECHO_BF16 or ECHO_F16");
-    const int64_t chunks = chunks_of(numel, n_tensors, NORM_CHUNK);
+    int64_t chunk;
+    const int64_t chunks = norm_chunks(numel, n_tensors, &chunk);
     if (chunks < 0 || (n_tensors > 0 && !grads)) return refuse(ECHO_EINVAL, "bad sizes");
     if (!out_norm || misaligned(out_norm, 4)) return refuse(ECHO_EINVAL, "out_norm is NULL or not aligned");
     for (int i = 0; i < n_tensors; ++i)
@@ -189,6 +200,7 @@ int echo_grad_norm(const void *const *grads, const int64_t *numel, int32_t n_ten
     hipStream_t st = (hipStream_t)stream;
     return queue([&] {
       NormTensors t;
+      t.chunk = chunk;
       int64_t done = 0;
       for (int i = 0; i < n_tensors;) {
         t.n = 0;
@@ -197,7 +209,7 @@ int echo_grad_norm(const void *const *grads, const int64_t *numel, int32_t n_ten
           if (numel[i] == 0) continue;
           t.grad[t.n] = grads[i];
           t.numel[t.n] = numel[i];
-          t.chunk0[t.n + 1] = t.chunk0[t.n] + (uint32_t)((numel[i] + NORM_CHUNK - 1) / NORM_CHUNK);
+          t.chunk0[t.n + 1] = t.chunk0[t.n] + (uint32_t)((numel[i] + chunk - 1) / chunk);
           ++t.n;
         }
         if (t.n) launch_grad_norm(t, dtype, partial + done, st);
@@ -250,6 +262,7 @@ int echo_adamw_step(const echo_adamw_args *a, void *stream) {
     c.eps = (float)a->eps;
     c.step = (uint32_t)a->step;
     c.seed = a->seed;
+    c.moderate = c.eps >= 0x1p-60f && c.eps <= 0x1p30f && c.root <= 0x1p40f;
     return queue([&] {
       StepTensors t;
       int64_t state0 = 0;

@@ -1,6 +1,9 @@
 // The update (include/echo_learner.h): norm of many gradients, one AdamW step over many tensors.
+#include <type_traits>
+
 #include "echo_device.h"
 #include "learner_kernels.h"
+#include "update_math.h"
 #include "../../include/echo_learner.h"
 
 namespace echo {
@@ -18,65 +21,99 @@ __device__ __forceinline__ int tensor_of(const uint32_t *chunk0, int n, uint32_t
   return lo;
 }
 
-template <int DT> __device__ __forceinline__ float get(const void *p, int64_t i) {
-  if (DT == ECHO_BF16) return bf16_bits_to_f32(((const uint16_t *)p)[i]);
-  if (DT == ECHO_F16) return (float)((const _Float16 *)p)[i];
-  return ((const float *)p)[i];
+// Four elements of a tensor at any element's alignment, or those of them before its end.
+template <int DT, bool WHOLE = false, typename I = int64_t> __device__ __forceinline__ void load4(f32x4 &v, const void *p, I i, I n) {
+  if (WHOLE || i + 4 <= n) {
+    if constexpr (DT == ECHO_F32) __builtin_memcpy(&v, (const float *)p + i, 16);
+    else {
+      uint32_t q[2];
+      __builtin_memcpy(q, (const uint16_t *)p + i, 8);
+      if constexpr (DT == ECHO_BF16) v = f32x4{__uint_as_float(q[0] << 16), __uint_as_float(q[0] & 0xffff0000u), __uint_as_float(q[1] << 16), __uint_as_float(q[1] & 0xffff0000u)};
+      else v = f32x4{h16_bits_to_f32((uint16_t)q[0]), h16_bits_to_f32((uint16_t)(q[0] >> 16)), h16_bits_to_f32((uint16_t)q[1]), h16_bits_to_f32((uint16_t)(q[1] >> 16))};
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[k] = 0.f;
+    if (i + k < n) {
+      if constexpr (DT == ECHO_F32) v[k] = ((const float *)p)[i + k];
+      else if constexpr (DT == ECHO_BF16) v[k] = bf16_bits_to_f32(((const uint16_t *)p)[i + k]);
+      else v[k] = h16_bits_to_f32(((const uint16_t *)p)[i + k]);
+    }
+  }
+}
+template <bool WHOLE, typename T> __device__ __forceinline__ void store4(T *p, const T *v, int i, int n) {
+  if (WHOLE || i + 4 <= n) { __builtin_memcpy(p + i, v, 4 * sizeof(T)); return; }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (i + k < n) p[i + k] = v[k];
 }
 
-__device__ double block_sum(double v, double *sh) {
+template <int WAVES> __device__ double block_sum(double v, double *sh) {
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   if (threadIdx.x % 64 == 0) sh[threadIdx.x / 64] = v;
   __syncthreads();
   v = sh[0];
-  for (int i = 1; i < THREADS / 64; ++i) v += sh[i];
+  for (int i = 1; i < WAVES; ++i) v += sh[i];
   return v;
 }
 
+// A square of f32 is exact in f64, so the sum loses next to nothing and does not depend on sizes or order to within its rounding to f32.
 template <int DT> __global__ __launch_bounds__(THREADS) void norm_kernel(NormTensors t, double *partial) {
   __shared__ double sh[THREADS / 64];
+  constexpr int N = 8;
   const int i = tensor_of(t.chunk0, t.n, blockIdx.x);
-  const int64_t a = (int64_t)(blockIdx.x - t.chunk0[i]) * NORM_CHUNK, left = t.numel[i] - a, n = left < NORM_CHUNK ? left : NORM_CHUNK;
-  double s = 0;
-  for (int64_t j = threadIdx.x; j < n; j += THREADS) {
-    const double g = get<DT>(t.grad[i], a + j);
-    s = fma(g, g, s);
+  const int64_t a = (int64_t)(blockIdx.x - t.chunk0[i]) * t.chunk, end = min(t.numel[i], a + t.chunk);
+  double s[4] = {0, 0, 0, 0};
+  for (int64_t b = a; b < end; b += THREADS * 4 * N) {
+    f32x4 g[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) load4<DT>(g[u], t.grad[i], b + (u * THREADS + (int)threadIdx.x) * 4, end);
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[k] = fma((double)g[u][k], (double)g[u][k], s[k]);
   }
-  s = block_sum(s, sh);
-  if (threadIdx.x == 0) partial[blockIdx.x] = s;
+  const double all = block_sum<THREADS / 64>(s[0] + s[1] + s[2] + s[3], sh);
+  if (threadIdx.x == 0) partial[blockIdx.x] = all;
 }
 
-__global__ __launch_bounds__(THREADS) void norm_finish_kernel(const double *partial, int64_t n, float *out) {
-  __shared__ double sh[THREADS / 64];
-  double s = 0;
-  for (int64_t j = threadIdx.x; j < n; j += THREADS) s += partial[j];
-  s = block_sum(s, sh);
-  if (threadIdx.x == 0) *out = (float)sqrt(s);
+__global__ __launch_bounds__(1024) void norm_finish_kernel(const double *partial, int64_t n, float *out) {
+  __shared__ double sh[16];
+  double s[4] = {0, 0, 0, 0};
+  for (int64_t j = threadIdx.x; j < n; j += 4 * 1024)
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (j + u * 1024 < n) s[u] += partial[j + u * 1024];
+  const double all = block_sum<16>(s[0] + s[1] + s[2] + s[3], sh);
+  if (threadIdx.x == 0) *out = (float)sqrt(all);
 }
 
-// Magnitude and sign bits of an E4M3 code as f32 (codes 0x7f and 0xff are NaN).
-__device__ __forceinline__ float e4m3_value(uint32_t code) {
-  const uint32_t m = code & 0x7f;
-  const float f = m == 0x7f ? NAN : m >= 8 ? __uint_as_float((m + (120u << 3)) << 20) : (float)m * 0x1p-9f;
-  return code & 0x80 ? -f : f;
+// Four values as E4M3 codes, each the largest code not above value + unit * bits / 2^16, unit the distance of the codes around it (the hardware's conversion,
+// whose random bits are these at its field's top); a magnitude beyond 448, which a rounding of the scale can leave, counts as 448.
+__device__ __forceinline__ uint32_t e4m3_codes(const float *z, const uint32_t *bits_high) {
+  uint32_t q = 0;
+  float c[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    c[k] = __builtin_amdgcn_fmed3f(z[k], -448.0f, 448.0f);
+    if (z[k] != z[k]) c[k] = z[k];
+  }
+  q = __builtin_amdgcn_cvt_sr_fp8_f32(c[0], bits_high[0], q, 0);
+  q = __builtin_amdgcn_cvt_sr_fp8_f32(c[1], bits_high[1], q, 1);
+  q = __builtin_amdgcn_cvt_sr_fp8_f32(c[2], bits_high[2], q, 2);
+  q = __builtin_amdgcn_cvt_sr_fp8_f32(c[3], bits_high[3], q, 3);
+  return q & (((q & 0x7f7f7f7fu) + 0x7f7f7f7fu) | 0x7f7f7f7fu);   // no sign at a magnitude of 0
+}
+__device__ __forceinline__ f32x4 e4m3_values(uint32_t codes, float scale) {
+  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(codes, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(codes, true);
+  return f32x4{a[0] * scale, a[1] * scale, b[0] * scale, b[1] * scale};
 }
 
-// z in [0, 448] (a rounding above at most, or NaN) to the code below or above it, by 16 random bits: in f32 the three significand bits that stay end at
-// bit 20, so adding the random bits below them and cutting carries with the right probability; below 2^-6 codes are multiples of 2^-9.
-__device__ __forceinline__ uint32_t e4m3_code(float z, uint32_t bits) {
-  if (z != z) return 0x7f;
-  z = fminf(z, 448.0f);
-  uint32_t code;
-  if (z < 0x1p-6f) code = (uint32_t)floorf(z * 512.0f + (float)bits * 0x1p-16f);
-  else code = ((__float_as_uint(z) + (bits << 4)) >> 20) - (120u << 3);
-  return code < 0x7eu ? code : 0x7eu;
-}
-
-// A bf16 next to f, by 16 random bits; infinities and NaN stay what they are.
-__device__ __forceinline__ uint16_t bf16_by_chance(float f, uint32_t bits) {
-  const uint32_t u = __float_as_uint(f);
-  if ((u & 0x7f800000u) == 0x7f800000u) return f32_to_bf16_bits(f);
-  return (uint16_t)((u + bits) >> 16);
+// A bf16 next to f, by 16 random bits, in the high half; infinities and NaN stay what they are.
+__device__ __forceinline__ uint32_t bf16_by_chance(float f, uint32_t word) {
+  return f != f ? 0x7fc00000u : __float_as_uint(f) + (word & 0xffff);
 }
 
 // Scale of a block whose largest magnitude is `top`, and its reciprocal (0 for a block without weight).
@@ -87,9 +124,155 @@ __device__ __forceinline__ float block_scale(float top, float &inv) {
   return scale;
 }
 
-// A wave takes 256 consecutive elements, a lane four of them: one call of the generator, one block of the 8-bit states.
-template <int PT, int GT, int ST> __global__ __launch_bounds__(THREADS) void adamw_kernel(StepTensors t, StepConstants c) {
+// Random words of the four elements from s on.  What is the same for a whole wave (the high half of the counter, the step, what the first round makes of
+// them) is the scalar unit's.
+__device__ __forceinline__ u32x4 draws(int64_t s, uint32_t purpose, const StepConstants &c) {
+  return philox4x32_10((uint32_t)(s >> 2), __builtin_amdgcn_readfirstlane((uint32_t)(s >> 34)), c.step, purpose, (uint32_t)c.seed, (uint32_t)(c.seed >> 32));
+}
+
+// The largest value of a wave, in every lane: four steps within rows of 16 lanes, two between them, none through LDS.
+__device__ __forceinline__ float max_of_wave(float v) {
+#define STEP(ctrl) v = fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), ctrl, 0xf, 0xf, false)))
+  STEP(0xB1);    // the neighbour in pairs
+  STEP(0x4E);    // pairs of pairs
+  STEP(0x141);   // mirrored halves of a row
+  STEP(0x140);   // mirrored rows
+#undef STEP
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float of_lane(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
+
+// A workgroup's chunk.  A wave takes 256 consecutive elements at a time, a lane four of them: one call of the generator, one block of the 8-bit
+// states.  All that a thread reads is on its way before it computes.  WHOLE: the chunk ends inside the tensor.
+template <int PT, int GT, int ST, bool WHOLE> __device__ __forceinline__ void step_chunk(const StepTensors &t, const StepConstants &c, int i, int64_t a, float factor) {
 #pragma clang fp contract(off)
+  constexpr int N = STEP_CHUNK / (THREADS * 4);
+  typedef typename std::conditional<PT == ECHO_F32, float, uint16_t>::type Param;
+  typedef typename std::conditional<GT == ECHO_F32, float, uint16_t>::type Grad;
+  typedef typename std::conditional<ST == ECHO_F32, float, uint8_t>::type State;
+  const int left = WHOLE ? (int)STEP_CHUNK : (int)(t.numel[i] - a);
+  const int64_t s0 = t.state0[i] + a;
+  const float decay = t.decay[i];
+  Param *param = (Param *)t.param[i] + a;
+  const Grad *grad = (const Grad *)t.grad[i] + a;
+  uint16_t *snapshot = t.snapshot[i] ? t.snapshot[i] + a : nullptr;
+  State *ms_ = (State *)c.m + s0, *vs_ = (State *)c.v + s0;
+  float *m_scale = nullptr, *v_scale = nullptr;
+  if constexpr (ST != ECHO_F32) { m_scale = c.m_scale + s0 / ECHO_ADAMW_BLOCK; v_scale = c.v_scale + s0 / ECHO_ADAMW_BLOCK; }
+  const uint32_t mine = threadIdx.x * 4;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  f32x4 P[N], G[N], M[N], V[N];
+  uint32_t Mc[N], Vc[N];
+  float Ms[N], Vs[N];
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const uint32_t b = u * THREADS * 4 + mine;
+    if (!WHOLE && (int)b - lane * 4 >= left) break;   // (whole waves)
+    load4<PT, WHOLE, int>(P[u], param, b, left);
+    load4<GT, WHOLE, int>(G[u], grad, b, left);
+    if constexpr (ST == ECHO_F32) {
+      M[u] = *(const f32x4 *)(ms_ + b);
+      V[u] = *(const f32x4 *)(vs_ + b);
+    } else {
+      Mc[u] = *(const uint32_t *)(ms_ + b);
+      Vc[u] = *(const uint32_t *)(vs_ + b);
+      Ms[u] = m_scale[u * (THREADS / 64) + wave];
+      Vs[u] = v_scale[u * (THREADS / 64) + wave];
+    }
+  }
+  // Averages first; are all of them moderate?
+  uint32_t far = 0;
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const uint32_t b = u * THREADS * 4 + mine;
+    if (!WHOLE && (int)b - lane * 4 >= left) break;
+    if constexpr (ST != ECHO_F32) {
+      M[u] = e4m3_values(Mc[u], Ms[u]);
+      V[u] = e4m3_values(Vc[u], Vs[u]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float g = G[u][k] * factor;
+      M[u][k] = M[u][k] * c.beta1 + g * c.fresh1;
+      V[u][k] = V[u][k] * c.beta2 + g * c.fresh2 * g;
+      if (!WHOLE && (int)b + k >= left) M[u][k] = V[u][k] = 0.f;
+      far = max(far, max(beyond_moderate(M[u][k]), beyond_moderate(V[u][k])));
+    }
+  }
+  const bool moderate = c.moderate && __all(far < MODERATE_SPAN);
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const uint32_t b = u * THREADS * 4 + mine;
+    if (!WHOLE && (int)b - lane * 4 >= left) break;
+    float p[4], over[4];
+    if (moderate) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) over[k] = moderate_quotient(M[u][k], moderate_sqrt(V[u][k]) * c.root + c.eps);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) over[k] = M[u][k] / (sqrtf(V[u][k]) * c.root + c.eps);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) p[k] = P[u][k] * decay - over[k] * c.size;
+    if constexpr (PT == ECHO_F32) {
+      store4<WHOLE>(param, p, b, left);
+      if (snapshot) {
+        uint16_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = __builtin_bit_cast(uint16_t, (__bf16)p[k]);
+        store4<WHOLE>(snapshot, w, b, left);
+      }
+    } else {
+      const u32x4 r = draws(s0 + b, 1, c);
+      const uint32_t q[4] = {bf16_by_chance(p[0], r.x), bf16_by_chance(p[1], r.y), bf16_by_chance(p[2], r.z), bf16_by_chance(p[3], r.w)};
+      const uint32_t pairs[2] = {__builtin_amdgcn_perm(q[1], q[0], 0x07060302u), __builtin_amdgcn_perm(q[3], q[2], 0x07060302u)};
+      uint16_t w[4];
+      __builtin_memcpy(w, pairs, 8);
+      store4<WHOLE>(param, w, b, left);
+    }
+    if constexpr (ST == ECHO_F32) {
+      *(f32x4 *)(ms_ + b) = M[u];
+      *(f32x4 *)(vs_ + b) = V[u];
+    }
+  }
+  if constexpr (ST != ECHO_F32) {
+    // The scales of the wave's blocks, a lane each: one division for all of them.
+    float top = 0.f, inv;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const float mt = max_of_wave(fmaxf(fmaxf(fabsf(M[u][0]), fabsf(M[u][1])), fmaxf(fabsf(M[u][2]), fabsf(M[u][3]))));
+      const float vt = max_of_wave(fmaxf(fmaxf(V[u][0], V[u][1]), fmaxf(V[u][2], V[u][3])));
+      top = lane == 2 * u ? mt : lane == 2 * u + 1 ? vt : top;
+    }
+    const float scale = block_scale(top, inv);
+    if (lane < 2 * N && (WHOLE || (lane / 2 * THREADS + wave * 64) * 4 < left)) (lane % 2 ? v_scale : m_scale)[lane / 2 * (THREADS / 64) + wave] = scale;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const uint32_t b = u * THREADS * 4 + mine;
+      if (!WHOLE && (int)b - lane * 4 >= left) break;
+      const u32x4 r = draws(s0 + b, 0, c);
+      const uint32_t low[4] = {r.x << 16, r.y << 16, r.z << 16, r.w << 16}, high[4] = {r.x & 0xffff0000u, r.y & 0xffff0000u, r.z & 0xffff0000u, r.w & 0xffff0000u};
+      const float mi = of_lane(inv, 2 * u), vi = of_lane(inv, 2 * u + 1);
+      float z[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) z[k] = M[u][k] * mi;
+      *(uint32_t *)(ms_ + b) = e4m3_codes(z, low);
+      // a positive v at the least code's value has that code whatever the bits
+      const float least = vi > 0.f ? 0x1p-9f : 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        z[k] = V[u][k] * vi;
+        if (V[u][k] > 0.f && z[k] < least) z[k] = least;
+      }
+      *(uint32_t *)(vs_ + b) = e4m3_codes(z, high);
+    }
+  }
+}
+
+template <int PT, int GT, int ST> __global__ __launch_bounds__(THREADS) void adamw_kernel(StepTensors t, StepConstants c) {
   float factor = 1.0f;
   if (c.norm) {
     const float norm = *c.norm;
@@ -97,55 +280,9 @@ template <int PT, int GT, int ST> __global__ __launch_bounds__(THREADS) void ada
     if (norm > c.max_norm) factor = c.max_norm / norm;
   }
   const int i = tensor_of(t.chunk0, t.n, blockIdx.x);
-  const int64_t n = t.numel[i], a = (int64_t)(blockIdx.x - t.chunk0[i]) * STEP_CHUNK, s0 = t.state0[i];
-  const float decay = t.decay[i];
-  for (int64_t b = a + threadIdx.x * 4; b < a + STEP_CHUNK; b += THREADS * 4) {
-    if (b - threadIdx.x % 64 * 4 >= n) break;   // (whole waves)
-    const int64_t s = s0 + b;
-    float m[4], v[4];
-    if (ST == ECHO_F32) {
-      const f32x4 m4 = *(const f32x4 *)((const float *)c.m + s), v4 = *(const f32x4 *)((const float *)c.v + s);
-      for (int k = 0; k < 4; ++k) { m[k] = m4[k]; v[k] = v4[k]; }
-    } else {
-      const uint32_t m4 = *(const uint32_t *)((const uint8_t *)c.m + s), v4 = *(const uint32_t *)((const uint8_t *)c.v + s);
-      const float ms = c.m_scale[s / ECHO_ADAMW_BLOCK], vs = c.v_scale[s / ECHO_ADAMW_BLOCK];
-      for (int k = 0; k < 4; ++k) { m[k] = e4m3_value(m4 >> 8 * k & 0xff) * ms; v[k] = e4m3_value(v4 >> 8 * k & 0xff) * vs; }
-    }
-    u32x4 by_chance = {0, 0, 0, 0};
-    if (PT == ECHO_BF16) by_chance = philox4x32_10((uint32_t)(s >> 2), (uint32_t)(s >> 34), c.step, 1, (uint32_t)c.seed, (uint32_t)(c.seed >> 32));
-    const uint32_t rp[4] = {by_chance.x, by_chance.y, by_chance.z, by_chance.w};
-    for (int k = 0; k < 4; ++k) {
-      const bool in = b + k < n;
-      if (!in) { m[k] = 0.f; v[k] = 0.f; continue; }
-      const float g = get<GT>(t.grad[i], b + k) * factor;
-      m[k] = m[k] * c.beta1 + g * c.fresh1;
-      v[k] = v[k] * c.beta2 + g * c.fresh2 * g;
-      const float p = get<PT>(t.param[i], b + k) * decay - m[k] / (sqrtf(v[k]) * c.root + c.eps) * c.size;
-      if (PT == ECHO_F32) ((float *)t.param[i])[b + k] = p;
-      else ((uint16_t *)t.param[i])[b + k] = bf16_by_chance(p, rp[k] & 0xffff);
-      if (PT == ECHO_F32 && t.snapshot[i]) t.snapshot[i][b + k] = f32_to_bf16_bits(p);
-    }
-    if (ST == ECHO_F32) {
-      *(f32x4 *)((float *)c.m + s) = f32x4{m[0], m[1], m[2], m[3]};
-      *(f32x4 *)((float *)c.v + s) = f32x4{v[0], v[1], v[2], v[3]};
-    } else {
-      const u32x4 r = philox4x32_10((uint32_t)(s >> 2), (uint32_t)(s >> 34), c.step, 0, (uint32_t)c.seed, (uint32_t)(c.seed >> 32));
-      const uint32_t rs[4] = {r.x, r.y, r.z, r.w};
-      float mi, vi;
-      const float ms = block_scale(wave_max(fmaxf(fmaxf(fabsf(m[0]), fabsf(m[1])), fmaxf(fabsf(m[2]), fabsf(m[3])))), mi);
-      const float vs = block_scale(wave_max(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]))), vi);
-      uint32_t m4 = 0, v4 = 0;
-      for (int k = 0; k < 4; ++k) {
-        uint32_t mc = e4m3_code(fabsf(m[k]) * mi, rs[k] & 0xffff), vc = e4m3_code(v[k] * vi, rs[k] >> 16);
-        if (m[k] < 0.f && mc) mc |= 0x80;
-        if (v[k] > 0.f && vs > 0.f && !vc) vc = 1;
-        m4 |= mc << 8 * k; v4 |= vc << 8 * k;
-      }
-      *(uint32_t *)((uint8_t *)c.m + s) = m4;
-      *(uint32_t *)((uint8_t *)c.v + s) = v4;
-      if (threadIdx.x % 64 == 0) { c.m_scale[s / ECHO_ADAMW_BLOCK] = ms; c.v_scale[s / ECHO_ADAMW_BLOCK] = vs; }
-    }
-  }
+  const int64_t a = (int64_t)(blockIdx.x - t.chunk0[i]) * STEP_CHUNK;
+  if (a + STEP_CHUNK <= t.numel[i]) step_chunk<PT, GT, ST, true>(t, c, i, a, factor);
+  else step_chunk<PT, GT, ST, false>(t, c, i, a, factor);
 }
 
 template <int PT, int GT> void launch_states(const StepTensors &t, const StepConstants &c, int state_dtype, hipStream_t st) {
@@ -162,7 +299,7 @@ void launch_grad_norm(const NormTensors &t, int dtype, double *partial, hipStrea
   else if (dtype == ECHO_BF16) norm_kernel<ECHO_BF16><<<grid, THREADS, 0, st>>>(t, partial);
   else norm_kernel<ECHO_F16><<<grid, THREADS, 0, st>>>(t, partial);
 }
-void launch_norm_finish(const double *partial, int64_t n, float *out, hipStream_t st) { norm_finish_kernel<<<1, THREADS, 0, st>>>(partial, n, out); }
+void launch_norm_finish(const double *partial, int64_t n, float *out, hipStream_t st) { norm_finish_kernel<<<1, 1024, 0, st>>>(partial, n, out); }
 
 void launch_adamw(const StepTensors &t, const StepConstants &c, int param_dtype, int grad_dtype, int state_dtype, hipStream_t st) {
   if (param_dtype == ECHO_F32) {

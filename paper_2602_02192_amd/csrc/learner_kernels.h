@@ -41,6 +41,7 @@ struct NormTensors {
   int64_t numel[TENSORS_PER_LAUNCH];
   uint32_t chunk0[TENSORS_PER_LAUNCH + 1];   // first chunk of each tensor
   int32_t n;
+  int64_t chunk;                             // elements of a workgroup
 };
 struct StepTensors {
   void *param[TENSORS_PER_LAUNCH];
@@ -59,8 +60,11 @@ struct StepConstants {
   float max_norm, beta1, fresh1, beta2, fresh2, root, eps, size;   // fresh: 1 - beta; root: (1 - beta2^t)^-1/2; size: lr / (1 - beta1^t)
   uint32_t step;
   uint64_t seed;
+  bool moderate;   // eps and root keep the denominators of moderate averages within 2^-60 .. 2^90
 };
-constexpr int64_t NORM_CHUNK = 16384, STEP_CHUNK = 4096;   // elements of a workgroup
+constexpr int64_t STEP_CHUNK = 4096;          // elements of a workgroup
+// Elements of a workgroup of the norm: enough of them to fill the GPU, and, of many elements, few enough partial sums for the one workgroup that adds them up.
+inline int64_t norm_chunk(int64_t elements) { return elements < (int64_t)1 << 26 ? 8192 : 65536; }
 void launch_grad_norm(const NormTensors &t, int dtype, double *partial, hipStream_t st);          // partial[chunk]
 void launch_norm_finish(const double *partial, int64_t n, float *out, hipStream_t st);
 void launch_adamw(const StepTensors &t, const StepConstants &c, int param_dtype, int grad_dtype, int state_dtype, hipStream_t st);

@@ -203,6 +203,34 @@ def test_zero_gradients_and_tiny_ones(learner):
         assert torch.isfinite(p[0]).all() and (p[0][300:] == 1).all()
 
 
+def test_square_root_and_quotient_bit_for_bit():
+    import os
+    import subprocess
+    from paper_2602_02192_amd import build
+    if not os.path.exists(build.UPDATE_SWEEP):
+        build.build_sweep()
+    r = subprocess.run([build.UPDATE_SWEEP], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and r.stdout.split() == ["roots", "0", "reciprocals", "0", "quotients", "0"], r.stdout + r.stderr
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-18, 1e-13, 1e-3, 1e12, 1e18])
+def test_averages_of_every_size(learner, scale):
+    """From squares that vanish in f32 to squares near its end: the bits of the operations as written, whichever form computes them."""
+    n = 5000
+    r = np.random.default_rng(2)
+    gn = (r.normal(0, 1, n) * np.exp(r.normal(0, 3, n)) * scale).astype(np.float32)
+    gn[::7] = 0
+    gn[4096:4400] = 0
+    for eps, root in ((1e-8, 0.999), (1e-30, 0.999), (1e-8, 0.0)):
+        p, g = [torch.ones(n, device="cuda")], [torch.from_numpy(gn).cuda()]
+        m, v = torch.zeros(5120, device="cuda"), torch.zeros(5120, device="cuda")
+        hyper = dict(lr=1e-3, beta1=0.9, beta2=root, eps=eps)
+        learner.adamw_step(p, g, m, v, step=1, **hyper)
+        want = plain.adamw(np.ones(n, np.float32), gn, np.zeros(n, np.float32), np.zeros(n, np.float32), 0.0, step=1, factor=1.0, **hyper)
+        for got, ref in zip((p[0], m[:n], v[:n]), want):
+            assert np.array_equal(host(got), ref)
+
+
 def test_state_dict_and_graph(learner):
     p, g, _ = problem([5000, 77], 8, grads="bf16", params="bf16")
     opt = learner.AdamW(p, lr=1e-3, state_dtype=torch.float8_e4m3fn, seed=3, max_norm=1.0)
