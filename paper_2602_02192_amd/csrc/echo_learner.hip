@@ -50,7 +50,7 @@ const char *wrong_logits(const echo_logits *x) {
   const size_t e = element_bytes(x->dtype);
   if (!e) return "logits must be ECHO_F32, ECHO_BF16 or ECHO_F16";
   if (x->rows < 0 || x->rows > INT32_MAX) return "rows must lie in 0 .. 2^31 - 1";
-  if (x->vocab < 1 || x->vocab > 1 << 30) return "vocab must lie in 1 .. 2^30";
+  if (x->vocab < 1 || x->vocab > 1 << 28) return "vocab must lie in 1 .. 2^28";
   if (x->rows * ((x->vocab + 8191) / 8192) > INT32_MAX) return "rows * vocab exceeds what one call takes (2^44)";
   if (x->row_stride < x->vocab) return "row_stride is less than vocab";
   if (x->rows > 0 && x->row_stride > INT64_MAX / 16 / x->rows) return "rows * row_stride is out of range";

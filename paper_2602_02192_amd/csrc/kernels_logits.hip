@@ -8,7 +8,8 @@ namespace echo {
 namespace {
 
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
-constexpr int THREADS = 256, BATCH = 8;   // vectors of 16 bytes that a thread holds at a time
+constexpr int THREADS = 256;
+constexpr int FEW = 2, MANY = 8;   // vectors of 16 bytes that a thread holds at a time
 constexpr int CANDIDATES = 1024;
 
 typedef uint32_t vec16 __attribute__((ext_vector_type(4)));
@@ -48,33 +49,43 @@ template <int DT> __device__ __forceinline__ vec16 filled(float f) {
   return pack<DT>(v);
 }
 
-// Vectors of a row: rows of any stride start at any element, so these are loads and stores of 16 bytes at the elements' alignment.  A vector that
-// passes the end is filled up with -inf, and stored element by element.
-template <int DT> __device__ __forceinline__ vec16 load_vector(const typename Elem<DT>::type *x, int j, int end) {
+// A row in vectors of 16 bytes, at the elements' alignment since rows of any stride start at any element.  Where the entries do not fill the vectors, the second
+// one begins before the first one's end: vector 0 repeats entries of vector 1, which count and are written there.  (A row has a vector's entries at least.)
+struct Vectors { int count, repeated; };
+template <int DT> __device__ __forceinline__ Vectors vectors_of(int vocab) {
   constexpr int VEC = Elem<DT>::VEC;
+  const int n = (vocab + VEC - 1) / VEC;
+  return {n, n * VEC - vocab};
+}
+template <int DT> __device__ __forceinline__ uint32_t byte_of(int entry) { return (uint32_t)entry * (uint32_t)sizeof(typename Elem<DT>::type); }
+template <int DT> __device__ __forceinline__ int entry_of(const Vectors &r, int v) { return max(v * Elem<DT>::VEC - r.repeated, 0); }
+template <int DT> __device__ __forceinline__ vec16 load_vector(const typename Elem<DT>::type *x, const Vectors &r, int v) {
   vec16 q;
-  if (j + VEC <= end) { __builtin_memcpy(&q, x + j, 16); return q; }
-  q = filled<DT>(-INFINITY);
-  if (j < end) {
-    typename Elem<DT>::type e[VEC];
-    __builtin_memcpy(e, &q, 16);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i)
-      if (j + i < end) e[i] = x[j + i];
-    __builtin_memcpy(&q, e, 16);
-  }
+  __builtin_memcpy(&q, (const char *)x + byte_of<DT>(entry_of<DT>(r, min(v, r.count - 1))), 16);
   return q;
 }
-template <int DT> __device__ __forceinline__ void store_vector(typename Elem<DT>::type *x, int j, int end, const vec16 &q) {
-  constexpr int VEC = Elem<DT>::VEC;
-  if (j + VEC <= end) { __builtin_memcpy(x + j, &q, 16); return; }
-  if (j < end) {
-    typename Elem<DT>::type e[VEC];
+template <int DT> __device__ __forceinline__ void store_vector(typename Elem<DT>::type *x, const Vectors &r, int v, const vec16 &q) {
+  if (v == 0 && r.repeated) {
+    typename Elem<DT>::type e[Elem<DT>::VEC];
     __builtin_memcpy(e, &q, 16);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i)
-      if (j + i < end) x[j + i] = e[i];
+    for (int i = 0; i < Elem<DT>::VEC - 1; ++i)
+      if (i < Elem<DT>::VEC - r.repeated) x[i] = e[i];
+  } else if (v < r.count) __builtin_memcpy((char *)x + byte_of<DT>(entry_of<DT>(r, v)), &q, 16);
+}
+// Vector 0 with -inf in place of the entries it repeats.
+template <int DT> __device__ __forceinline__ vec16 own_entries(vec16 q, int repeated) {
+  constexpr int VEC = Elem<DT>::VEC;
+  const vec16 none = filled<DT>(-INFINITY);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (VEC == 4) q[i] = i >= VEC - repeated ? none[i] : q[i];
+    else {
+      if (2 * i >= VEC - repeated) q[i] = (q[i] & 0xffff0000u) | (none[i] & 0xffffu);
+      if (2 * i + 1 >= VEC - repeated) q[i] = (q[i] & 0xffffu) | (none[i] & 0xffff0000u);
+    }
   }
+  return q;
 }
 
 __device__ __forceinline__ bool row_live(const LogitRows &r, int64_t t) {
@@ -127,31 +138,44 @@ __device__ __forceinline__ float logprob(float x, const RowStats &s, float inv_t
   return x == -INFINITY && s.sum == s.sum ? -INFINITY : (x - s.top) * inv_t - LN2 * log2f(s.sum);
 }
 
-// Adds the entries of N vectors to a thread's statistics.
-template <int DT, int N> __device__ __forceinline__ float largest(const vec16 *q, float *of_vector = nullptr) {
-  float top = -INFINITY;
+template <int DT> __device__ __forceinline__ float largest(const vec16 &q) {
+  float m = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < Elem<DT>::VEC; ++e) m = fmaxf(m, element<DT>(q, e));
+  return m;
+}
+template <int DT> __device__ __forceinline__ void add_entries(RowStats &s, const vec16 &q, float from, float c) {
+#pragma unroll
+  for (int e = 0; e < Elem<DT>::VEC; ++e) {
+    const float d = (element<DT>(q, e) - from) * c, p = __builtin_amdgcn_exp2f(d);
+    s.sum += p;
+    s.turn = fmaf(p, fmaxf(d, -200.f), s.turn);
+  }
+}
+// Adds N vectors a thread, vector v of the first thread and those W apart, to a thread's statistics; what does not count (from `end` on, or repeated) becomes -inf.
+template <int DT, int W, int N> __device__ __forceinline__ void add_vectors(RowStats &s, vec16 *q, const Vectors &r, int v, int end, float c, float *of_vector = nullptr) {
+  if (v + N * W > end) {
+    const vec16 none = filled<DT>(-INFINITY);
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[u][i] = v + u * W + (int)threadIdx.x < end ? q[u][i] : none[i];
+  }
+  if (v == 0 && r.repeated && threadIdx.x == 0) q[0] = own_entries<DT>(q[0], r.repeated);
+  float top = s.top;
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    float m = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < Elem<DT>::VEC; ++e) m = fmaxf(m, element<DT>(q[u], e));
+    as_loaded(q[u]);
+    const float m = largest<DT>(q[u]);
     if (of_vector) of_vector[u] = m;
     top = fmaxf(top, m);
   }
-  return top;
-}
-template <int DT, int N> __device__ __forceinline__ void add_entries(RowStats &s, vec16 *q, float top, float c) {
   s = moved(s, top, c);
   const float from = top == -INFINITY ? 0.f : top;
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     as_loaded(q[u]);
-#pragma unroll
-    for (int e = 0; e < Elem<DT>::VEC; ++e) {
-      const float d = (element<DT>(q[u], e) - from) * c, p = __builtin_amdgcn_exp2f(d);
-      s.sum += p;
-      s.turn = fmaf(p, fmaxf(d, -200.f), s.turn);
-    }
+    add_entries<DT>(s, q[u], from, c);
   }
 }
 
@@ -159,54 +183,82 @@ template <int DT, int N> __device__ __forceinline__ void add_entries(RowStats &s
 struct RowPart { RowStats s; float given; };
 struct Parts { RowPart *part; uint64_t *top; };   // [rows, splits], [rows, splits, top_k]
 
-// The k largest of n <= CANDIDATES keys (different ones but for 0), in order, by their rank among all; what is left of out is 0.
+// The k largest of n <= CANDIDATES different keys, in order, by their rank among all; what is left of out is 0.
 __device__ __forceinline__ void select_top(const uint64_t *keys, int n, int k, uint64_t *out) {
   for (int i = threadIdx.x; i < n; i += THREADS) {
     const uint64_t mine = keys[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += keys[j] > mine || (keys[j] == mine && j < i);
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) rank += keys[j] > mine;
     if (rank < k) out[rank] = mine;
   }
   for (int i = n + threadIdx.x; i < k; i += THREADS) out[i] = 0;
 }
+// Sixteen bits that the leading sixteen of at least k of a wave's lanes reach: the k-th largest of them, by bisection (0 for k beyond the lanes).
+__device__ __forceinline__ uint32_t reached_by(uint32_t leading, int k) {
+  uint32_t low = 0;
+#pragma unroll
+  for (int b = 15; b >= 0; --b) {
+    const uint32_t tried = low | 1u << b;
+    if (__popcll(__ballot(leading >= tried)) >= k) low = tried;
+  }
+  return low;
+}
 
-template <int DT, bool TOP> __global__ __launch_bounds__(THREADS) void stats_kernel(LogitRows r, Parts p, int splits, int span, int top_k) {
+// What is written for a row, by one thread each.
+__device__ __forceinline__ void write_stats(const RowOutputs &out, int64_t t, bool live, const RowStats &s, float given, float inv_t) {
+  if (out.logprobs) out.logprobs[t] = live ? logprob(given, s, inv_t) : 0.f;
+  if (out.entropy) out.entropy[t] = live ? stats_entropy(s) : 0.f;
+  if (out.lse) out.lse[t] = live ? stats_lse(s, inv_t) : 0.f;
+}
+__device__ __forceinline__ void write_top(const RowOutputs &out, int64_t t, int i, bool live, const RowStats &s, uint64_t key, float inv_t) {
+  out.top_ids[t * out.top_k + i] = key ? key_index(key) : -1;
+  out.top_logprobs[t * out.top_k + i] = !live ? 0.f : key ? logprob(key_value(key), s, inv_t) : -INFINITY;
+}
+
+// One part of a row.  ONE: it is all of the row, and the outputs are written here.
+template <int DT, int BATCH, bool TOP, bool ONE> __global__ __launch_bounds__(THREADS) void stats_kernel(LogitRows r, Parts p, int splits, int span, RowOutputs outputs) {
   constexpr int VEC = Elem<DT>::VEC;
   __shared__ RowStats sh[THREADS / 64];
   const int64_t t = blockIdx.x / (uint32_t)splits;
   const int part = blockIdx.x % (uint32_t)splits;
-  if (!row_live(r, t)) return;
+  const int top_k = outputs.top_k;
+  if (!row_live(r, t)) {
+    if constexpr (ONE) {
+      if (threadIdx.x == 0) write_stats(outputs, t, false, {}, 0.f, 0.f);
+      for (int i = threadIdx.x; i < top_k; i += THREADS) write_top(outputs, t, i, false, {}, 0, 0.f);
+    }
+    return;
+  }
   const auto *x = (const typename Elem<DT>::type *)r.x + t * r.stride;
   const float c = LOG2E / r.temperature;
-  const int begin = part * span, end = min(r.vocab, begin + span);
+  const Vectors row = vectors_of<DT>(r.vocab);
+  const int begin = part * span, end = min(row.count, begin + span);   // vectors
   RowStats s = {-INFINITY, 0.f, 0.f};
   vec16 q[BATCH];
   float of_vector[BATCH];
 #pragma unroll
   for (int u = 0; u < BATCH; ++u) of_vector[u] = -INFINITY;
-  for (int j = begin + threadIdx.x * VEC; j - (int)threadIdx.x * VEC < end; j += THREADS * VEC * BATCH) {
+  for (int v = begin; v < end; v += THREADS * BATCH) {
 #pragma unroll
-    for (int u = 0; u < BATCH; ++u) q[u] = load_vector<DT>(x, j + u * THREADS * VEC, end);
-    add_entries<DT, BATCH>(s, q, fmaxf(s.top, largest<DT, BATCH>(q, of_vector)), c);
+    for (int u = 0; u < BATCH; ++u) q[u] = load_vector<DT>(x, row, v + u * THREADS + threadIdx.x);
+    add_vectors<DT, THREADS, BATCH>(s, q, row, v, end, c, TOP ? of_vector : nullptr);
   }
   const float mine = s.top;
   s = block_stats<THREADS / 64>(s, c, sh);
   if (threadIdx.x == 0) {
-    const int given = r.targets ? r.targets[t] : -1;
-    p.part[blockIdx.x] = {s, given >= begin && given < end ? widen<DT>(x[given]) : -INFINITY};
+    const int given = r.targets ? r.targets[t] : -1, first_entry = entry_of<DT>(row, begin), last_entry = entry_of<DT>(row, end);
+    const float logit = given >= first_entry && given < last_entry ? widen<DT>(x[given]) : -INFINITY;
+    if constexpr (ONE) write_stats(outputs, t, true, s, logit, 1.0f / r.temperature);
+    else p.part[blockIdx.x] = {s, logit};
   }
   if constexpr (TOP) {   // (the part is one batch: it is still in q)
     __shared__ uint64_t keys[CANDIDATES];
     __shared__ uint32_t bound[THREADS / 64], count;
-    uint64_t *out = p.top + (int64_t)blockIdx.x * top_k;
-    // A value that at least top_k entries of a wave reach: its lanes' largest entries, cut to 16 bits, by bisection.
-    const uint32_t key = order_bits(mine) >> 16;
-    uint32_t low = 0;
-#pragma unroll
-    for (int b = 15; b >= 0; --b) {
-      const uint32_t tried = low | 1u << b;
-      if (__popcll(__ballot(key >= tried)) >= top_k) low = tried;
-    }
+    __shared__ uint64_t best_here[ONE ? ECHO_TOP_MAX : 1];
+    uint64_t *out = ONE ? best_here : p.top + (int64_t)blockIdx.x * top_k;
+    // A value that at least top_k entries of a wave reach, since that many of its lanes' largest do.
+    uint32_t low = reached_by(order_bits(mine) >> 16, top_k);
     if (threadIdx.x % 64 == 0) bound[threadIdx.x / 64] = low;
     if (threadIdx.x == 0) count = 0;
     __syncthreads();
@@ -223,25 +275,21 @@ template <int DT, bool TOP> __global__ __launch_bounds__(THREADS) void stats_ker
         const float v = element<DT>(q[u], e);
         if (v >= floor) {
           const uint32_t at = atomicAdd(&count, 1u);
-          if (at < CANDIDATES) keys[at] = order_key(v, begin + (u * THREADS + (int)threadIdx.x) * VEC + e);
+          if (at < CANDIDATES) keys[at] = order_key(v, entry_of<DT>(row, begin + u * THREADS + (int)threadIdx.x) + e);
         }
       }
     }
     __syncthreads();
-    if (count <= CANDIDATES) return select_top(keys, count, top_k, out);
-    // Too many equal ones: one entry after the other, each the largest below the last.
+    const bool few = count <= CANDIDATES;
+    if (few) select_top(keys, count, top_k, out);
+    // Too many of them (equal logits): read once more, one entry after the other, each the largest below the last.
     uint64_t last = ~0ull;
-    for (int k = 0; k < top_k; ++k) {
+    for (int k = 0; k < top_k && !few; ++k) {
       uint64_t best = 0;
-#pragma unroll
-      for (int u = 0; u < BATCH; ++u) {
-        as_loaded(q[u]);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const float v = element<DT>(q[u], e);
-          const uint64_t key = order_key(v, begin + (u * THREADS + (int)threadIdx.x) * VEC + e);
-          if (v >= floor && key < last && key > best) best = key;
-        }
+      for (int j = entry_of<DT>(row, begin) + threadIdx.x; j < entry_of<DT>(row, end); j += THREADS) {
+        const float v = widen<DT>(x[j]);
+        const uint64_t key = order_key(v, j);
+        if (v >= floor && key < last && key > best) best = key;
       }
       for (int o = 32; o > 0; o >>= 1) { const uint64_t b = __shfl_xor(best, o, 64); best = b > best ? b : best; }
       __syncthreads();
@@ -251,6 +299,10 @@ template <int DT, bool TOP> __global__ __launch_bounds__(THREADS) void stats_ker
       for (int i = 0; i < THREADS / 64; ++i) best = max(best, keys[i]);
       if (threadIdx.x == 0) out[k] = best;
       last = best;
+    }
+    if constexpr (ONE) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < top_k; i += THREADS) write_top(outputs, t, i, true, s, best_here[i], 1.0f / r.temperature);
     }
   }
 }
@@ -278,42 +330,43 @@ template <bool TOP> __global__ __launch_bounds__(THREADS) void stats_finish_kern
     RowPart m = {{0.f, 0.f, 0.f}, 0.f};
     if (live) m = joined(p.part + t * splits, splits, LOG2E / r.temperature);
     if (threadIdx.x == 0) {
-      if (out.logprobs) out.logprobs[t] = live ? logprob(m.given, m.s, inv_t) : 0.f;
-      if (out.entropy) out.entropy[t] = live ? stats_entropy(m.s) : 0.f;
-      if (out.lse) out.lse[t] = live ? stats_lse(m.s, inv_t) : 0.f;
+      write_stats(out, t, live, m.s, m.given, inv_t);
       all = m.s;
     }
   }
   if constexpr (TOP) {
-    // The parts' lists, as many at a time as fit: of the best so far and of the new ones only those count that reach the last of a list, since that many
-    // entries are as large as it is.
-    __shared__ uint64_t keys[CANDIDATES], best[ECHO_TOP_MAX], bound;
-    __shared__ uint32_t count;
-    const int k = out.top_k, n = splits * k, at_once = (CANDIDATES / k - 1) * k;
+    // The parts' lists, as many keys at a time as fit beside the best so far.  Of all these only those count that reach a value which at least k of a wave's
+    // lanes reach.
+    constexpr int HELD = CANDIDATES / THREADS;
+    __shared__ uint64_t keys[CANDIDATES], best[ECHO_TOP_MAX];
+    __shared__ uint32_t bound[THREADS / 64], count;
+    const int k = out.top_k, n = splits * k;
     const uint64_t *lists = p.top + t * n;
-    if (threadIdx.x == 0) { bound = 1; count = 0; }
-    __syncthreads();
-    for (int done = 0; live && done < n; done += at_once) {
-      const int more = min(n - done, at_once);
-      for (int i = threadIdx.x; i < more / k; i += THREADS) atomicMax((unsigned long long *)&bound, lists[done + i * k + k - 1]);
-      __syncthreads();
-      const uint64_t least = bound;
-      for (int i = threadIdx.x; i < more; i += THREADS) {
-        const uint64_t key = lists[done + i];
-        if (key >= least) keys[atomicAdd(&count, 1u)] = key;
+    for (int done = 0, have = 0; live && done < n; done += CANDIDATES - have, have = k) {
+      const int more = min(n - done, CANDIDATES - have);
+      uint64_t held[HELD], top = 0;
+#pragma unroll
+      for (int u = 0; u < HELD; ++u) {
+        const int i = u * THREADS + threadIdx.x;
+        held[u] = i < more ? lists[done + i] : i < more + have ? best[i - more] : 0;
+        top = max(top, held[u]);
       }
-      if (done && threadIdx.x < k && best[threadIdx.x] >= least) keys[atomicAdd(&count, 1u)] = best[threadIdx.x];
+      const uint32_t low = reached_by((uint32_t)(top >> 48), k);
+      if (threadIdx.x % 64 == 0) bound[threadIdx.x / 64] = low;
+      if (threadIdx.x == 0) count = 0;
+      __syncthreads();
+      uint64_t least = 1;
+#pragma unroll
+      for (int i = 0; i < THREADS / 64; ++i) least = max(least, (uint64_t)bound[i] << 48);
+#pragma unroll
+      for (int u = 0; u < HELD; ++u)
+        if (held[u] >= least) keys[atomicAdd(&count, 1u)] = held[u];
       __syncthreads();
       select_top(keys, count, k, best);
       __syncthreads();
-      if (threadIdx.x == 0) { bound = max(best[k - 1], (uint64_t)1); count = 0; }
-      __syncthreads();
     }
-    __syncthreads();
     for (int i = threadIdx.x; i < k; i += THREADS) {
-      const uint64_t key = live ? best[i] : 0;
-      out.top_ids[t * k + i] = key ? key_index(key) : -1;
-      out.top_logprobs[t * k + i] = !live ? 0.f : key ? logprob(key_value(key), all, inv_t) : -INFINITY;
+      write_top(out, t, i, live, all, live ? best[i] : 0, inv_t);
     }
   }
 }
@@ -380,14 +433,19 @@ __device__ __forceinline__ void no_loss(const LossOutputs &out, int64_t t) {
 }
 
 struct GivenStats { const float *lse, *entropy, *g, *h; };   // g, h nullable
+__device__ __forceinline__ RowGrad given_grad(const GivenStats &given, int64_t t, float inv_t) {
+  const float h = given.h ? given.h[t] : 0.f;
+  return row_grad(inv_t, given.lse[t], LOG2E, 1.f, 0.f, given.g ? given.g[t] : 0.f, h, given.h ? given.entropy[t] : 0.f, inv_t);
+}
 
 // One batch of a row's gradient: from given statistics (LOSS false), or from the parts of stats_kernel, which every workgroup of a row joins while its
 // vectors are on their way.
 template <int DT, bool LOSS> __global__ __launch_bounds__(THREADS) void grad_kernel(LogitRows r, GivenStats given, PolicyTerms terms, Parts p, int splits, LossOutputs out,
                                                                                  int batches) {
-  constexpr int VEC = Elem<DT>::VEC;
+  constexpr int BATCH = MANY;
   const int64_t t = blockIdx.x / (uint32_t)batches;
-  const int j = (int)(blockIdx.x % (uint32_t)batches) * THREADS * VEC * BATCH + threadIdx.x * VEC;
+  const Vectors row = vectors_of<DT>(r.vocab);
+  const int begin = (int)(blockIdx.x % (uint32_t)batches) * (THREADS * BATCH);
   const bool first = blockIdx.x % (uint32_t)batches == 0;
   const auto *x = (const typename Elem<DT>::type *)r.x + t * r.stride;
   auto *o = (typename Elem<DT>::type *)out.grad + t * out.stride;
@@ -396,12 +454,13 @@ template <int DT, bool LOSS> __global__ __launch_bounds__(THREADS) void grad_ker
   if (!live) {
     if (LOSS && first && threadIdx.x == 0) no_loss(out, t);
 #pragma unroll
-    for (int u = 0; u < BATCH; ++u) store_vector<DT>(o, j + u * THREADS * VEC, r.vocab, vec16{0, 0, 0, 0});
+    for (int u = 0; u < BATCH; ++u)
+      store_vector<DT>(o, row, begin + u * THREADS + threadIdx.x, vec16{0, 0, 0, 0});
     return;
   }
   vec16 q[BATCH];
 #pragma unroll
-  for (int u = 0; u < BATCH; ++u) q[u] = load_vector<DT>(x, j + u * THREADS * VEC, r.vocab);
+  for (int u = 0; u < BATCH; ++u) q[u] = load_vector<DT>(x, row, begin + u * THREADS + threadIdx.x);
   RowGrad c;
   int target = -1;
   if constexpr (LOSS) {
@@ -415,29 +474,29 @@ template <int DT, bool LOSS> __global__ __launch_bounds__(THREADS) void grad_ker
     c = sh;
     target = r.targets[t];
   } else {
-    const float inv_t = 1.0f / r.temperature, h = given.h ? given.h[t] : 0.f;
-    c = row_grad(inv_t, given.lse[t], LOG2E, 1.f, 0.f, given.g ? given.g[t] : 0.f, h, given.h ? given.entropy[t] : 0.f, inv_t);
+    c = given_grad(given, t, 1.0f / r.temperature);
     if (given.g) target = r.targets[t];
   }
 #pragma unroll
   for (int u = 0; u < BATCH; ++u) {
-    const int at = j + u * THREADS * VEC;
-    store_vector<DT>(o, at, r.vocab, grad_vector<DT>(q[u], target - at, c));
+    const int v = begin + u * THREADS + threadIdx.x;
+    as_loaded(q[u]);
+    store_vector<DT>(o, row, v, grad_vector<DT>(q[u], target - entry_of<DT>(row, v), c));
   }
 }
 
 // A whole row by one workgroup: its first N vectors a thread stay in registers between the statistics and the gradient, what is beyond them is read
 // again.
 template <int DT, int W, int N> __global__ __launch_bounds__(W) void loss_row_kernel(LogitRows r, PolicyTerms terms, LossOutputs out) {
-  constexpr int VEC = Elem<DT>::VEC, AGAIN = 4;
+  constexpr int AGAIN = 4, AT_ONCE = 4;
   __shared__ RowStats sh[W / 64];
   const int64_t t = blockIdx.x;
   const auto *x = (const typename Elem<DT>::type *)r.x + t * r.stride;
   auto *o = (typename Elem<DT>::type *)out.grad + t * out.stride;
-  const int mine = threadIdx.x * VEC;
+  const Vectors row = vectors_of<DT>(r.vocab);
   if (!token_live(r, terms, t)) {
     if (threadIdx.x == 0) no_loss(out, t);
-    for (int j = mine; j < r.vocab; j += W * VEC) store_vector<DT>(o, j, r.vocab, vec16{0, 0, 0, 0});
+    for (int v = threadIdx.x; v < row.count; v += W) store_vector<DT>(o, row, v, vec16{0, 0, 0, 0});
     return;
   }
   const float c = LOG2E / r.temperature;
@@ -445,32 +504,36 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W) void loss_row_ke
   const float given = widen<DT>(x[target]);
   vec16 q[N];
 #pragma unroll
-  for (int u = 0; u < N; ++u) q[u] = load_vector<DT>(x, mine + u * W * VEC, r.vocab);
+  for (int u = 0; u < N; ++u) q[u] = load_vector<DT>(x, row, u * W + threadIdx.x);
   RowStats s = {-INFINITY, 0.f, 0.f};
-  for (int j = N * W * VEC; j < r.vocab; j += AGAIN * W * VEC) {
+  // a few vectors at a time, as they arrive
+#pragma unroll
+  for (int u = 0; u + AT_ONCE <= N; u += AT_ONCE) add_vectors<DT, W, AT_ONCE>(s, q + u, row, u * W, row.count, c);
+  if constexpr (N % AT_ONCE != 0) add_vectors<DT, W, N % AT_ONCE>(s, q + N / AT_ONCE * AT_ONCE, row, N / AT_ONCE * AT_ONCE * W, row.count, c);
+  for (int v = N * W; v < row.count; v += AGAIN * W) {
     vec16 a[AGAIN];
 #pragma unroll
-    for (int u = 0; u < AGAIN; ++u) a[u] = load_vector<DT>(x, j + mine + u * W * VEC, r.vocab);
-    add_entries<DT, AGAIN>(s, a, fmaxf(s.top, largest<DT, AGAIN>(a)), c);
+    for (int u = 0; u < AGAIN; ++u) a[u] = load_vector<DT>(x, row, v + u * W + threadIdx.x);
+    add_vectors<DT, W, AGAIN>(s, a, row, v, row.count, c);
   }
-  add_entries<DT, N>(s, q, fmaxf(s.top, largest<DT, N>(q)), c);
   s = block_stats<W / 64>(s, c, sh);   // (its barrier: the target's logit has been read before any gradient is written)
   const RowGrad g = finish_loss(r, terms, out, t, s, given, threadIdx.x == 0);
-  for (int j = N * W * VEC; j < r.vocab; j += AGAIN * W * VEC) {
+  for (int v = N * W; v < row.count; v += AGAIN * W) {
     vec16 a[AGAIN];
 #pragma unroll
-    for (int u = 0; u < AGAIN; ++u) a[u] = load_vector<DT>(x, j + mine + u * W * VEC, r.vocab);
+    for (int u = 0; u < AGAIN; ++u) a[u] = load_vector<DT>(x, row, v + u * W + threadIdx.x);
 #pragma unroll
     for (int u = 0; u < AGAIN; ++u) {
-      const int at = j + mine + u * W * VEC;
-      store_vector<DT>(o, at, r.vocab, grad_vector<DT>(a[u], target - at, g));
+      const int w = v + u * W + threadIdx.x;
+      as_loaded(a[u]);
+      store_vector<DT>(o, row, w, grad_vector<DT>(a[u], target - entry_of<DT>(row, w), g));
     }
   }
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    const int at = mine + u * W * VEC;
+    const int w = u * W + threadIdx.x;
     as_loaded(q[u]);
-    store_vector<DT>(o, at, r.vocab, grad_vector<DT>(q[u], target - at, g));
+    store_vector<DT>(o, row, w, grad_vector<DT>(q[u], target - entry_of<DT>(row, w), g));
   }
 }
 
@@ -485,24 +548,90 @@ __global__ __launch_bounds__(64) void loss_finish_kernel(LogitRows r, PolicyTerm
   finish_loss(r, terms, out, t, m.s, m.given, threadIdx.x == 0);
 }
 
-// Parts of a row: one batch each where the top entries are wanted, a few batches otherwise.
-struct Split { int splits, span; };
-Split split_of(const LogitRows &x, bool top) {
-  const int vec = x.dtype == ECHO_F32 ? 4 : 8, batch = THREADS * vec * BATCH;
-  const int whole = batch * (top ? 1 : 4);
-  const int splits = (x.vocab + whole - 1) / whole;
-  const int span = ((x.vocab + splits - 1) / splits + vec - 1) / vec * vec;   // (at most `whole`)
-  return {splits, span};
+// Rows of less than a vector, a thread each.
+template <int DT> __global__ __launch_bounds__(THREADS) void narrow_kernel(LogitRows r, bool stats, RowOutputs outputs, bool loss, GivenStats given, PolicyTerms terms, LossOutputs out) {
+  const int64_t t = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+  if (t >= r.rows) return;
+  const auto *x = (const typename Elem<DT>::type *)r.x + t * r.stride;
+  const float inv_t = 1.0f / r.temperature, c = LOG2E / r.temperature;
+  const int target = r.targets ? r.targets[t] : -1;
+  bool live = row_live(r, t);
+  if (loss) live = token_live(r, terms, t);
+  RowStats s = {-INFINITY, 0.f, 0.f};
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    v[j] = live && j < r.vocab ? widen<DT>(x[j]) : -INFINITY;
+    s.top = fmaxf(s.top, v[j]);
+  }
+  const float from = s.top == -INFINITY ? 0.f : s.top;
+  float logit = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float d = (v[j] - from) * c, p = __builtin_amdgcn_exp2f(d);
+    s.sum += p;
+    s.turn = fmaf(p, fmaxf(d, -200.f), s.turn);
+    if (j == target) logit = v[j];
+  }
+  if (stats) {
+    write_stats(outputs, t, live, s, logit, inv_t);
+    uint64_t last = ~0ull;
+    for (int k = 0; k < outputs.top_k; ++k) {
+      uint64_t best = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint64_t key = live && v[j] > -INFINITY ? order_key(v[j], j) : 0;
+        if (key < last && key > best) best = key;
+      }
+      write_top(outputs, t, k, live, s, best, inv_t);
+      last = best;
+    }
+    return;
+  }
+  RowGrad g = {1.f, 0.f, 1.f, 0.f, 0.f, 0.f};
+  if (loss) {
+    if (live) g = finish_loss(r, terms, out, t, s, logit, true);
+    else no_loss(out, t);
+  } else if (live && given.lse[t] != -INFINITY) g = given_grad(given, t, inv_t);
+  else live = false;
+  if (!out.grad) return;
+  auto *o = (typename Elem<DT>::type *)out.grad + t * out.stride;
+  for (int j = 0; j < 8; ++j) {
+    if (j >= r.vocab) break;
+    const float d = fmaf(v[j], g.scale, -g.from) * g.unit, y = __builtin_amdgcn_exp2f(d) * fmaf(g.b, fmaxf(d, -200.f), g.a) + (j == target ? g.at_target : 0.f);
+    o[j] = narrow<DT>(live ? y : 0.f);
+  }
 }
-size_t parts_bytes(const LogitRows &x, const Split &s) { return ((size_t)x.rows * s.splits * sizeof(RowPart) + 255) / 256 * 256; }
+
+// Parts of a row: one batch each where the top entries are wanted, a few batches otherwise; of few rows small batches, so that there are parts for the
+// whole GPU.
+struct Split { int splits, span, batch; };   // span: vectors of a part
+int vector_entries(const LogitRows &x) { return x.dtype == ECHO_F32 ? 4 : 8; }
+int row_vectors(const LogitRows &x) { return (x.vocab + vector_entries(x) - 1) / vector_entries(x); }
+bool is_narrow(const LogitRows &x) { return x.vocab < vector_entries(x); }
+Split split_of(const LogitRows &x, bool top) {
+  const int n = row_vectors(x), large = THREADS * MANY * (top ? 1 : 4);
+  const int batch = n > THREADS * MANY && x.rows * ((n + large - 1) / large) < 256 ? FEW : MANY;
+  const int whole = THREADS * batch * (top || batch == FEW ? 1 : 4);
+  const int splits = (n + whole - 1) / whole;
+  return {splits, (n + splits - 1) / splits, batch};
+}
+size_t parts_bytes(const LogitRows &x, const Split &s) { return s.splits == 1 ? 0 : ((size_t)x.rows * s.splits * sizeof(RowPart) + 255) / 256 * 256; }
 
 }  // namespace
 
 size_t logprobs_workspace(const LogitRows &x, int top_k) {
   const Split s = split_of(x, top_k > 0);
-  return parts_bytes(x, s) + (size_t)x.rows * s.splits * top_k * sizeof(uint64_t);
+  return parts_bytes(x, s) + (s.splits == 1 ? 0 : (size_t)x.rows * s.splits * top_k * sizeof(uint64_t));
 }
-size_t policy_workspace(const LogitRows &x) { return parts_bytes(x, split_of(x, false)); }
+
+// Rows of at most a workgroup's registers are taken whole, in one launch; so are longer ones where there are enough to fill the GPU.
+static bool by_rows(const LogitRows &x) { return row_vectors(x) <= 256 * 8 || x.rows >= 200; }
+size_t policy_workspace(const LogitRows &x) {
+  // (without a gradient the loss is found from the parts)
+  const Split s = split_of(x, false);
+  return ((size_t)x.rows * s.splits * sizeof(RowPart) + 255) / 256 * 256;
+}
 
 #define FOR_DTYPE(dt, CALL)                                    \
   do {                                                         \
@@ -511,26 +640,37 @@ size_t policy_workspace(const LogitRows &x) { return parts_bytes(x, split_of(x, 
     else { constexpr int DT = ECHO_F16; CALL; }                \
   } while (0)
 
+template <typename... A> static void launch_narrow(const LogitRows &x, hipStream_t st, A... a) {
+  FOR_DTYPE(x.dtype, (narrow_kernel<DT><<<dim3((uint32_t)((x.rows + THREADS - 1) / THREADS)), THREADS, 0, st>>>(x, a...)));
+}
+template <int DT, int BATCH, bool ONE> static void launch_stats_of(const LogitRows &x, const Parts &p, const Split &s, const RowOutputs &out, hipStream_t st) {
+  const dim3 grid((uint32_t)(x.rows * s.splits));
+  if (out.top_k > 0) stats_kernel<DT, BATCH, true, ONE><<<grid, THREADS, 0, st>>>(x, p, s.splits, s.span, out);
+  else stats_kernel<DT, BATCH, false, ONE><<<grid, THREADS, 0, st>>>(x, p, s.splits, s.span, out);
+}
+static void launch_parts(const LogitRows &x, const Parts &p, const Split &s, const RowOutputs &out, hipStream_t st) {
+  if (s.batch == FEW) FOR_DTYPE(x.dtype, (launch_stats_of<DT, FEW, false>(x, p, s, out, st)));
+  else FOR_DTYPE(x.dtype, (launch_stats_of<DT, MANY, false>(x, p, s, out, st)));
+}
+
 void launch_token_logprobs(const LogitRows &x, const RowOutputs &out, void *workspace, hipStream_t st) {
+  if (is_narrow(x)) return launch_narrow(x, st, true, out, false, GivenStats{}, PolicyTerms{}, LossOutputs{});
   const Split s = split_of(x, out.top_k > 0);
   const Parts p = {(RowPart *)workspace, (uint64_t *)((char *)workspace + parts_bytes(x, s))};
-  const dim3 grid((uint32_t)(x.rows * s.splits));
-  if (out.top_k > 0) {
-    FOR_DTYPE(x.dtype, (stats_kernel<DT, true><<<grid, THREADS, 0, st>>>(x, p, s.splits, s.span, out.top_k)));
-    stats_finish_kernel<true><<<dim3((uint32_t)x.rows), THREADS, 0, st>>>(x, p, s.splits, out);
-  } else {
-    FOR_DTYPE(x.dtype, (stats_kernel<DT, false><<<grid, THREADS, 0, st>>>(x, p, s.splits, s.span, 0)));
-    stats_finish_kernel<false><<<dim3((uint32_t)x.rows), 64, 0, st>>>(x, p, s.splits, out);
+  if (s.splits == 1) {
+    FOR_DTYPE(x.dtype, (launch_stats_of<DT, MANY, true>(x, p, s, out, st)));
+    return;
   }
+  launch_parts(x, p, s, out, st);
+  if (out.top_k > 0) stats_finish_kernel<true><<<dim3((uint32_t)x.rows), THREADS, 0, st>>>(x, p, s.splits, out);
+  else stats_finish_kernel<false><<<dim3((uint32_t)x.rows), 64, 0, st>>>(x, p, s.splits, out);
 }
-static int grad_batches(const LogitRows &x) {
-  const int batch = THREADS * (x.dtype == ECHO_F32 ? 4 : 8) * BATCH;
-  return (x.vocab + batch - 1) / batch;
-}
+static int grad_batches(const LogitRows &x) { return (row_vectors(x) + THREADS * MANY - 1) / (THREADS * MANY); }
 void launch_token_logprobs_grad(const LogitRows &x, const float *lse, const float *entropy, const float *g, const float *h, void *out, int64_t out_stride,
                                 hipStream_t st) {
   const int batches = grad_batches(x);
   const LossOutputs o = {nullptr, nullptr, nullptr, out, out_stride};
+  if (is_narrow(x)) return launch_narrow(x, st, false, RowOutputs{}, false, GivenStats{lse, entropy, g, h}, PolicyTerms{}, o);
   FOR_DTYPE(x.dtype, (grad_kernel<DT, false><<<dim3((uint32_t)(x.rows * batches)), THREADS, 0, st>>>(x, GivenStats{lse, entropy, g, h}, PolicyTerms{}, Parts{}, 0, o, batches)));
 }
 void launch_policy_loss(const LogitRows &x, const PolicyTerms &terms, float *loss, float *logprobs, float *entropy, void *grad, int64_t grad_stride, void *workspace,
@@ -538,11 +678,16 @@ void launch_policy_loss(const LogitRows &x, const PolicyTerms &terms, float *los
   const Split s = split_of(x, false);
   const Parts p = {(RowPart *)workspace, nullptr};
   const LossOutputs o = {loss, logprobs, entropy, grad, grad_stride};
-  if (grad && x.rows >= 200) {
-    FOR_DTYPE(x.dtype, (loss_row_kernel<DT, 1024, DT == ECHO_F32 ? 17 : 19><<<dim3((uint32_t)x.rows), 1024, 0, st>>>(x, terms, o)));
+  if (is_narrow(x)) return launch_narrow(x, st, false, RowOutputs{}, true, GivenStats{}, terms, o);
+  if (grad && by_rows(x)) {
+    const dim3 grid((uint32_t)x.rows);
+    if (row_vectors(x) <= 256 * 8) FOR_DTYPE(x.dtype, (loss_row_kernel<DT, 256, 8><<<grid, 256, 0, st>>>(x, terms, o)));
+    else if (row_vectors(x) <= 512 * 8) FOR_DTYPE(x.dtype, (loss_row_kernel<DT, 512, 8><<<grid, 512, 0, st>>>(x, terms, o)));
+    else if (row_vectors(x) <= 1024 * 10) FOR_DTYPE(x.dtype, (loss_row_kernel<DT, 1024, 10><<<grid, 1024, 0, st>>>(x, terms, o)));
+    else FOR_DTYPE(x.dtype, (loss_row_kernel<DT, 1024, DT == ECHO_F32 ? 17 : 19><<<grid, 1024, 0, st>>>(x, terms, o)));
     return;
   }
-  FOR_DTYPE(x.dtype, (stats_kernel<DT, false><<<dim3((uint32_t)(x.rows * s.splits)), THREADS, 0, st>>>(x, p, s.splits, s.span, 0)));
+  launch_parts(x, p, s, RowOutputs{}, st);
   if (!grad) {
     loss_finish_kernel<<<dim3((uint32_t)x.rows), 64, 0, st>>>(x, terms, p, s.splits, o);
     return;

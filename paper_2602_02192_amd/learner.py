@@ -7,9 +7,10 @@ refuses raise echo.EchoError, tensors that it could not be handed (another type,
 from __future__ import annotations
 
 import ctypes as C
+import operator
+import struct
 from typing import NamedTuple, Optional, Sequence
 
-import numpy as np
 import torch
 
 from .echo import ECHO_BF16, ECHO_F32, EchoError, lib
@@ -31,8 +32,8 @@ class _LossOpts(C.Structure):
     _fields_ = [(n, C.c_float) for n in ("clip_low", "clip_high", "ratio_cap", "sampler_cap", "kl_coef", "entropy_coef")]
 
 
-class _AdamW(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("params", "grads", "snapshot", "numel", "weight_decay", "m", "v", "m_scale", "v_scale", "norm")] + \
+class _AdamW(C.Structure):   # (host arrays are bytes, packed in one go)
+    _fields_ = [(n, C.c_char_p) for n in ("params", "grads", "snapshot", "numel", "weight_decay")] + [(n, C.c_void_p) for n in ("m", "v", "m_scale", "v_scale", "norm")] + \
                [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps")] + [("step", C.c_int64), ("seed", C.c_uint64), ("max_norm", C.c_float)] + \
                [(n, C.c_int32) for n in ("n_tensors", "param_dtype", "grad_dtype", "state_dtype")]
 
@@ -60,50 +61,71 @@ def _chk(rc: int) -> None:
         raise EchoError(rc, lib.echo_last_error(None).decode())
 
 
-class _on:
-    """The stream of a call on `device`, with that device current."""
+class _current:
+    """Makes GPU `index` the current one where it is not."""
 
-    def __init__(self, device: torch.device):
-        if device.type != "cuda":
-            raise ValueError(f"tensors must live on a GPU, got {device}")
-        self.index = device.index
+    def __init__(self, index: int):
+        self.index = index
 
     def __enter__(self):
         self.before = torch.cuda.current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream(self.index).cuda_stream
+        torch.cuda.set_device(self.index)
 
     def __exit__(self, *exc):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
+        torch.cuda.set_device(self.before)
 
 
-def _vector(t: Optional[torch.Tensor], name: str, rows: int, like: torch.Tensor, dtype=torch.float32):
-    """Address of a contiguous [rows] tensor next to `like`; None stays None."""
+# (the handle alone: an object of torch.cuda.Stream for it costs as much as two launches)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _call(index: int, fn, *args) -> None:
+    """A call of the library on the current stream of GPU `index`, its last argument."""
+    if index < 0:
+        raise ValueError("tensors must live on a GPU")
+    if torch.cuda.current_device() == index:
+        rc = fn(*args, _raw_stream(index))
+    else:
+        with _current(index):
+            rc = fn(*args, _raw_stream(index))
+    if rc != 0:
+        _chk(rc)
+
+
+def _vector(t: Optional[torch.Tensor], name: str, rows: int, gpu: int, dtype=torch.float32):
+    """Address of a contiguous [rows] tensor on GPU `gpu`; None stays None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != rows or t.device != like.device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {rows} on {like.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.shape != (rows,) or t.get_device() != gpu or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {rows} on GPU {gpu}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
 def _matrix(t: torch.Tensor, name: str):
-    """Row stride of a two-dimensional tensor whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must have two dimensions and contiguous rows, got shape {tuple(t.shape)}, strides {t.stride()}")
-    if t.shape[0] <= 1:
-        return max(t.shape[1], 1)
-    if t.stride(0) < t.shape[1]:
-        raise ValueError(f"the rows of {name} overlap: stride {t.stride(0)} for {t.shape[1]} entries")
-    return t.stride(0)
+    """Rows, columns and row stride of a two-dimensional tensor whose rows are contiguous."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, got shape {tuple(t.shape)}")
+    (rows, columns), (stride, step) = t.shape, t.stride()
+    if columns > 1 and step != 1:
+        raise ValueError(f"the rows of {name} must be contiguous, got strides {t.stride()}")
+    if rows <= 1:
+        return rows, columns, max(columns, 1)
+    if stride < columns:
+        raise ValueError(f"the rows of {name} overlap: stride {stride} for {columns} entries")
+    return rows, columns, stride
 
 
-def _logits(x: torch.Tensor, targets, temperature: float) -> _Logits:
-    if x.dtype not in (torch.float32, torch.bfloat16, torch.float16):
+_LOGITS = {torch.float32: ECHO_F32, torch.bfloat16: ECHO_BF16, torch.float16: ECHO_F16}
+
+
+def _logits(x: torch.Tensor, targets, temperature: float):
+    """The description of the logits, their rows and their GPU."""
+    dtype = _LOGITS.get(x.dtype)
+    if dtype is None:
         raise ValueError(f"logits must be float32, bfloat16 or float16, got {x.dtype}")
-    stride = _matrix(x, "logits")
-    return _Logits(x.data_ptr(), _vector(targets, "targets", x.shape[0], x, torch.int32), x.shape[0], stride, x.shape[1], _DTYPE[x.dtype], temperature)
+    rows, vocab, stride = _matrix(x, "logits")
+    gpu = x.get_device()
+    return _Logits(x.data_ptr(), _vector(targets, "targets", rows, gpu, torch.int32), rows, stride, vocab, dtype, temperature), rows, gpu
 
 
 def _workspace(nbytes: int, like: torch.Tensor):
@@ -126,17 +148,19 @@ class TokenLogprobs(NamedTuple):
 
 
 def _token_logprobs(logits, targets, temperature, top_k) -> TokenLogprobs:
-    x = _logits(logits, targets, temperature)
-    rows, dev = logits.shape[0], logits.device
-    with _on(dev) as stream:
-        f = torch.empty(3 if targets is not None else 2, rows, dtype=torch.float32, device=dev)
-        ids = torch.empty(rows, top_k, dtype=torch.int32, device=dev) if top_k > 0 else None
-        tops = torch.empty(rows, top_k, dtype=torch.float32, device=dev) if top_k > 0 else None
-        need = lib.echo_token_logprobs_workspace(C.byref(x), top_k)
-        ws = _workspace(need, logits)
-        entropy, lse = f[0], f[1]
-        logprobs = f[2] if targets is not None else None
-        _chk(lib.echo_token_logprobs(C.byref(x), top_k, _addr(logprobs), entropy.data_ptr(), lse.data_ptr(), _addr(ids), _addr(tops), _addr(ws), need, stream))
+    x, rows, gpu = _logits(logits, targets, temperature)
+    dev = logits.device
+    entropy, lse, logprobs = torch.empty((3, rows), dtype=torch.float32, device=dev).unbind()
+    if targets is None:
+        logprobs = None
+    ids = tops = None
+    if top_k > 0:
+        ids = torch.empty((rows, top_k), dtype=torch.int32, device=dev)
+        tops = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
+    xp = C.byref(x)
+    need = lib.echo_token_logprobs_workspace(xp, top_k)
+    ws = _workspace(need, logits)
+    _call(gpu, lib.echo_token_logprobs, xp, top_k, _addr(logprobs), entropy.data_ptr(), lse.data_ptr(), _addr(ids), _addr(tops), _addr(ws), need)
     return TokenLogprobs(logprobs, entropy, lse, ids, tops)
 
 
@@ -173,12 +197,10 @@ def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor], l
                         grad_entropy: Optional[torch.Tensor] = None, *, temperature: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of sum(grad_logprobs * logprobs + grad_entropy * entropy) with respect to the logits, from what token_logprobs returned.
     `out` may be the logits themselves."""
-    x = _logits(logits, targets, temperature)
-    rows = logits.shape[0]
-    a = [_vector(t, n, rows, logits) for t, n in ((lse, "lse"), (entropy, "entropy"), (grad_logprobs, "grad_logprobs"), (grad_entropy, "grad_entropy"))]
-    with _on(logits.device) as stream:
-        out = _grad_like(logits, out)
-        _chk(lib.echo_token_logprobs_grad(C.byref(x), *a, out.data_ptr(), _matrix(out, "out"), stream))
+    x, rows, gpu = _logits(logits, targets, temperature)
+    a = [_vector(t, n, rows, gpu) for t, n in ((lse, "lse"), (entropy, "entropy"), (grad_logprobs, "grad_logprobs"), (grad_entropy, "grad_entropy"))]
+    out = _grad_like(logits, out)
+    _call(gpu, lib.echo_token_logprobs_grad, C.byref(x), *a, out.data_ptr(), _matrix(out, "out")[2])
     return out
 
 
@@ -207,49 +229,50 @@ def policy_loss(logits: torch.Tensor, targets: torch.Tensor, advantages: torch.T
     """The paper's clipped objective token by token, and d sum(loss) / d logits: `logits.backward(result.grad_logits)` carries it on into
     the network.  `weights` [rows] scale the tokens (1 / tokens of the batch for a mean); a token of weight 0 takes no part.
     `grad_out` may be the logits themselves."""
-    x = _logits(logits, targets, temperature)
-    rows, dev = logits.shape[0], logits.device
-    a = [_vector(t, n, rows, logits) for t, n in ((advantages, "advantages"), (old_logprobs, "old_logprobs"), (weights, "weights"),
-                                                  (sampler_logprobs, "sampler_logprobs"), (ref_logprobs, "ref_logprobs"))]
+    x, rows, gpu = _logits(logits, targets, temperature)
+    a = [_vector(advantages, "advantages", rows, gpu), _vector(old_logprobs, "old_logprobs", rows, gpu), _vector(weights, "weights", rows, gpu),
+         _vector(sampler_logprobs, "sampler_logprobs", rows, gpu), _vector(ref_logprobs, "ref_logprobs", rows, gpu)]
     o = _LossOpts(clip_low, clip_high, ratio_cap, sampler_cap, kl_coef, entropy_coef)
-    with _on(dev) as stream:
-        f = torch.empty(3, rows, dtype=torch.float32, device=dev)
-        grad = _grad_like(logits, grad_out) if want_grad or grad_out is not None else None
-        need = lib.echo_policy_loss_workspace(C.byref(x))
-        ws = _workspace(need, logits)
-        loss, logprobs, entropy = f[0], f[1], f[2]
-        _chk(lib.echo_policy_loss(C.byref(x), *a, C.byref(o), loss.data_ptr(), logprobs.data_ptr(), entropy.data_ptr(), _addr(grad),
-                                  0 if grad is None else _matrix(grad, "grad_out"), _addr(ws), need, stream))
+    loss, logprobs, entropy = torch.empty((3, rows), dtype=torch.float32, device=logits.device).unbind()
+    grad, stride = None, 0
+    if want_grad or grad_out is not None:
+        grad = _grad_like(logits, grad_out)
+        stride = _matrix(grad, "grad_out")[2]
+    xp = C.byref(x)
+    need = lib.echo_policy_loss_workspace(xp)
+    ws = _workspace(need, logits)
+    _call(gpu, lib.echo_policy_loss, xp, *a, C.byref(o), loss.data_ptr(), logprobs.data_ptr(), entropy.data_ptr(), _addr(grad), stride, _addr(ws), need)
     return PolicyLoss(loss, logprobs, entropy, grad)
 
 
 # ---- the update -----------------------------------------------------------------------------------------------------------------
 
+_dtype_of, _T = operator.attrgetter("dtype"), torch.Tensor
+
+
 def _same(tensors: Sequence[torch.Tensor], name: str, dtypes):
-    """(addresses, sizes) of contiguous tensors of one type on one device."""
+    """Addresses and sizes (as arrays of 64-bit numbers in bytes), type and GPU of contiguous tensors of one type on one device."""
     if not tensors:
         raise ValueError(f"no {name}")
-    dtype, device = tensors[0].dtype, tensors[0].device
+    dtype, gpu, n = tensors[0].dtype, tensors[0].get_device(), len(tensors)
     if dtype not in dtypes:
         raise ValueError(f"{name} must be of a type among {dtypes}, got {dtype}")
-    for i, t in enumerate(tensors):
-        if t.dtype != dtype or t.device != device or not t.is_contiguous():
-            raise ValueError(f"{name}[{i}] must be contiguous, {dtype} and on {device}")
-    return np.array([t.data_ptr() for t in tensors], np.uint64), np.array([t.numel() for t in tensors], np.int64)
+    if len(set(map(_dtype_of, tensors))) > 1 or len(set(map(_T.get_device, tensors))) > 1 or not all(map(_T.is_contiguous, tensors)):
+        raise ValueError(f"{name} must be contiguous, of one type and on one device")
+    return struct.pack(f"{n}Q", *map(_T.data_ptr, tensors)), struct.pack(f"{n}q", *map(_T.numel, tensors)), dtype, gpu
 
 
 def grad_norm(grads: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Euclidean norm of all the gradients together: a float32 tensor of one value on their GPU (`out`, or a new one)."""
-    addresses, numel = _same(grads, "grads", (torch.float32, torch.bfloat16, torch.float16))
-    like = grads[0]
-    with _on(like.device) as stream:
-        if out is None:
-            out = torch.empty((), dtype=torch.float32, device=like.device)
-        elif out.dtype != torch.float32 or out.numel() != 1 or out.device != like.device:
-            raise ValueError("out must be one float32 value on the gradients' device")
-        need = lib.echo_grad_norm_workspace(numel.ctypes.data, len(grads))
-        ws = _workspace(need, like)
-        _chk(lib.echo_grad_norm(addresses.ctypes.data, numel.ctypes.data, len(grads), _DTYPE[like.dtype], out.data_ptr(), _addr(ws), need, stream))
+    addresses, numel, dtype, gpu = _same(grads, "grads", (torch.float32, torch.bfloat16, torch.float16))
+    like, n = grads[0], len(grads)
+    if out is None:
+        out = torch.empty((), dtype=torch.float32, device=like.device)
+    elif out.dtype is not torch.float32 or out.numel() != 1 or out.get_device() != gpu:
+        raise ValueError("out must be one float32 value on the gradients' device")
+    need = lib.echo_grad_norm_workspace(numel, n)
+    ws = _workspace(need, like)
+    _call(gpu, lib.echo_grad_norm, addresses, numel, n, _DTYPE[dtype], out.data_ptr(), _addr(ws), need)
     return out
 
 
@@ -266,30 +289,30 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     number, or one per tensor.  `snapshot`: bfloat16 tensors that receive the new values of float32 parameters.  `norm` (from grad_norm):
     gradients are scaled to at most `max_norm`, and a norm that is not finite leaves everything as it is.  `seed` and `step` choose the random
     bits by which 8-bit states and bfloat16 parameters are rounded."""
-    pa, numel = _same(params, "params", (torch.float32, torch.bfloat16))
-    ga, gn = _same(grads, "grads", (torch.float32, torch.bfloat16))
-    like, dev = params[0], params[0].device
-    if not np.array_equal(gn, numel) or grads[0].device != dev:
+    pa, numel, ptype, gpu = _same(params, "params", (torch.float32, torch.bfloat16))
+    ga, gn, gtype, ggpu = _same(grads, "grads", (torch.float32, torch.bfloat16))
+    count = len(params)
+    if ggpu != gpu or gn != numel:
         raise ValueError("grads must match params in number, sizes and device")
     sa = None
     if snapshot is not None:
-        sa, sn = _same(snapshot, "snapshot", (torch.bfloat16,))
-        if not np.array_equal(sn, numel) or snapshot[0].device != dev:
+        sa, sn, _, sgpu = _same(snapshot, "snapshot", (torch.bfloat16,))
+        if sgpu != gpu or sn != numel:
             raise ValueError("snapshot must match params in number, sizes and device")
-    n = int((-(-numel // BLOCK)).sum()) * BLOCK
-    if m.dtype not in (torch.float32, torch.float8_e4m3fn):
-        raise ValueError(f"m and v must be float32 or float8_e4m3fn, got {m.dtype}")
-    ma, va = _vector(m, "m", n, like, m.dtype), _vector(v, "v", n, like, m.dtype)
-    msa, vsa = _vector(m_scale, "m_scale", n // BLOCK, like), _vector(v_scale, "v_scale", n // BLOCK, like)
-    if norm is not None and (norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != dev):
+    n = lib.echo_adamw_state_numel(numel, count)
+    states = m.dtype
+    if states is not torch.float32 and states is not torch.float8_e4m3fn:
+        raise ValueError(f"m and v must be float32 or float8_e4m3fn, got {states}")
+    ma, va = _vector(m, "m", n, gpu, states), _vector(v, "v", n, gpu, states)
+    msa, vsa = _vector(m_scale, "m_scale", n // BLOCK, gpu), _vector(v_scale, "v_scale", n // BLOCK, gpu)
+    if norm is not None and (norm.dtype is not torch.float32 or norm.numel() != 1 or norm.get_device() != gpu):
         raise ValueError("norm must be one float32 value on the parameters' device")
-    decay = np.full(len(params), weight_decay, np.float64) if isinstance(weight_decay, (int, float)) else np.array(weight_decay, np.float64)
-    if decay.shape != (len(params),):
-        raise ValueError(f"weight_decay must be one number or {len(params)}")
-    a = _AdamW(pa.ctypes.data, ga.ctypes.data, None if sa is None else sa.ctypes.data, numel.ctypes.data, decay.ctypes.data, ma, va, msa, vsa, _addr(norm),
-               lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, max_norm, len(params), _DTYPE[like.dtype], _DTYPE[grads[0].dtype], _DTYPE[m.dtype])
-    with _on(dev) as stream:
-        _chk(lib.echo_adamw_step(C.byref(a), stream))
+    decays = [weight_decay] * count if isinstance(weight_decay, (int, float)) else weight_decay
+    if len(decays) != count:
+        raise ValueError(f"weight_decay must be one number or {count}")
+    a = _AdamW(pa, ga, sa, numel, struct.pack(f"{count}d", *decays), ma, va, msa, vsa, _addr(norm), lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, max_norm,
+               count, _DTYPE[ptype], _DTYPE[gtype], _DTYPE[states])
+    _call(gpu, lib.echo_adamw_step, C.byref(a))
 
 
 class AdamW:
@@ -307,12 +330,11 @@ class AdamW:
         self.m_scale, self.v_scale = (torch.zeros(n // BLOCK, device=dev) for _ in range(2)) if state_dtype != torch.float32 else (None, None)
 
     def step(self, grads: Optional[Sequence[torch.Tensor]] = None) -> Optional[torch.Tensor]:
-        params = [p.detach() for p in self.params]
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if any(g is None for g in grads):
             raise ValueError("a parameter has no gradient")
         norm = grad_norm(grads) if self.max_norm != float("inf") else None
-        adamw_step(params, grads, self.m, self.v, step=self.steps + 1, lr=self.lr, beta1=self.betas[0], beta2=self.betas[1], eps=self.eps,
+        adamw_step(self.params, grads, self.m, self.v, step=self.steps + 1, lr=self.lr, beta1=self.betas[0], beta2=self.betas[1], eps=self.eps,
                    weight_decay=self.weight_decay, m_scale=self.m_scale, v_scale=self.v_scale, snapshot=self.snapshot, norm=norm, max_norm=self.max_norm,
                    seed=self.seed)
         self.steps += 1
