@@ -64,14 +64,19 @@ template <int DT> __device__ __forceinline__ vec16 load_vector(const typename El
   __builtin_memcpy(&q, (const char *)x + byte_of<DT>(entry_of<DT>(r, min(v, r.count - 1))), 16);
   return q;
 }
-template <int DT> __device__ __forceinline__ void store_vector(typename Elem<DT>::type *x, const Vectors &r, int v, const vec16 &q) {
+// ONCE: past the caches, which keep what is read again.
+template <int DT, bool ONCE = false> __device__ __forceinline__ void store_vector(typename Elem<DT>::type *x, const Vectors &r, int v, const vec16 &q) {
   if (v == 0 && r.repeated) {
     typename Elem<DT>::type e[Elem<DT>::VEC];
     __builtin_memcpy(e, &q, 16);
 #pragma unroll
     for (int i = 0; i < Elem<DT>::VEC - 1; ++i)
       if (i < Elem<DT>::VEC - r.repeated) x[i] = e[i];
-  } else if (v < r.count) __builtin_memcpy((char *)x + byte_of<DT>(entry_of<DT>(r, v)), &q, 16);
+  } else if (v < r.count) {
+    typedef vec16 __attribute__((aligned(2))) vec;
+    vec *to = (vec *)((char *)x + byte_of<DT>(entry_of<DT>(r, v)));
+    if (ONCE) __builtin_nontemporal_store(q, to); else *to = q;
+  }
 }
 // Vector 0 with -inf in place of the entries it repeats.
 template <int DT> __device__ __forceinline__ vec16 own_entries(vec16 q, int repeated) {
@@ -487,7 +492,7 @@ template <int DT, bool LOSS> __global__ __launch_bounds__(THREADS) void grad_ker
 
 // A whole row by one workgroup: its first N vectors a thread stay in registers between the statistics and the gradient, what is beyond them is read
 // again.
-template <int DT, int W, int N> __global__ __launch_bounds__(W) void loss_row_kernel(LogitRows r, PolicyTerms terms, LossOutputs out) {
+template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void loss_row_kernel(LogitRows r, PolicyTerms terms, LossOutputs out) {
   constexpr int AGAIN = 4, AT_ONCE = 4;
   __shared__ RowStats sh[W / 64];
   const int64_t t = blockIdx.x;
@@ -496,7 +501,7 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W) void loss_row_ke
   const Vectors row = vectors_of<DT>(r.vocab);
   if (!token_live(r, terms, t)) {
     if (threadIdx.x == 0) no_loss(out, t);
-    for (int v = threadIdx.x; v < row.count; v += W) store_vector<DT>(o, row, v, vec16{0, 0, 0, 0});
+    for (int v = threadIdx.x; v < row.count; v += W) store_vector<DT, true>(o, row, v, vec16{0, 0, 0, 0});
     return;
   }
   const float c = LOG2E / r.temperature;
@@ -526,14 +531,14 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W) void loss_row_ke
     for (int u = 0; u < AGAIN; ++u) {
       const int w = v + u * W + threadIdx.x;
       as_loaded(a[u]);
-      store_vector<DT>(o, row, w, grad_vector<DT>(a[u], target - entry_of<DT>(row, w), g));
+      store_vector<DT, true>(o, row, w, grad_vector<DT>(a[u], target - entry_of<DT>(row, w), g));
     }
   }
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     const int w = u * W + threadIdx.x;
     as_loaded(q[u]);
-    store_vector<DT>(o, row, w, grad_vector<DT>(q[u], target - entry_of<DT>(row, w), g));
+    store_vector<DT, true>(o, row, w, grad_vector<DT>(q[u], target - entry_of<DT>(row, w), g));
   }
 }
 
@@ -625,8 +630,9 @@ size_t logprobs_workspace(const LogitRows &x, int top_k) {
   return parts_bytes(x, s) + (s.splits == 1 ? 0 : (size_t)x.rows * s.splits * top_k * sizeof(uint64_t));
 }
 
-// Rows of at most a workgroup's registers are taken whole, in one launch; so are longer ones where there are enough to fill the GPU.
-static bool by_rows(const LogitRows &x) { return row_vectors(x) <= 256 * 8 || x.rows >= 200; }
+// Whether a workgroup takes a row whole, or several take parts of it and its gradient in two launches.  Short rows whole in any number; long ones where there are
+// enough to fill the GPU.  151936 entries, bf16: 64 rows 30 us whole, 20 in parts; 128 rows 31 and 31; 200 rows 33 and 41.  f32: 29 and 23, 36 and 40, 50 and 73.
+static bool by_rows(const LogitRows &x) { return row_vectors(x) <= 8192 || x.rows >= 128; }
 size_t policy_workspace(const LogitRows &x) {
   // (without a gradient the loss is found from the parts)
   const Split s = split_of(x, false);
@@ -681,10 +687,13 @@ void launch_policy_loss(const LogitRows &x, const PolicyTerms &terms, float *los
   if (is_narrow(x)) return launch_narrow(x, st, false, RowOutputs{}, true, GivenStats{}, terms, o);
   if (grad && by_rows(x)) {
     const dim3 grid((uint32_t)x.rows);
+    // Registers for short rows; two workgroups a CU, one of which waits for memory while the other computes, for long ones, of which they hold a part.  2048 rows of
+    // 9000 bf16: 24 us by 256 threads, 41 by 512; of 32000: 52 and 50, 86 with room for 18 vectors; of 151936: 298 by one workgroup a CU that holds the row, 264 by
+    // two that hold half.  In f32 a row is twice as long, and what is held counts for more: 494 by one that holds 45 %, 568 by two that hold 24 %.
     if (row_vectors(x) <= 256 * 8) FOR_DTYPE(x.dtype, (loss_row_kernel<DT, 256, 8><<<grid, 256, 0, st>>>(x, terms, o)));
     else if (row_vectors(x) <= 512 * 8) FOR_DTYPE(x.dtype, (loss_row_kernel<DT, 512, 8><<<grid, 512, 0, st>>>(x, terms, o)));
-    else if (row_vectors(x) <= 1024 * 10) FOR_DTYPE(x.dtype, (loss_row_kernel<DT, 1024, 10><<<grid, 1024, 0, st>>>(x, terms, o)));
-    else FOR_DTYPE(x.dtype, (loss_row_kernel<DT, 1024, DT == ECHO_F32 ? 17 : 19><<<grid, 1024, 0, st>>>(x, terms, o)));
+    else if (x.dtype != ECHO_F32 || row_vectors(x) <= 512 * 18) FOR_DTYPE(x.dtype, (loss_row_kernel<DT, 512, 18><<<grid, 512, 0, st>>>(x, terms, o)));
+    else loss_row_kernel<ECHO_F32, 1024, 17><<<grid, 1024, 0, st>>>(x, terms, o);
     return;
   }
   launch_parts(x, p, s, RowOutputs{}, st);
