@@ -4,6 +4,9 @@
 #include "learner_kernels.h"
 #include "../../include/echo_learner.h"
 
+// v_mul_legacy_f32, a product in which 0 times anything is 0 (the compiler has the instruction and no builtin for it).
+__device__ float mul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");
+
 namespace echo {
 namespace {
 
@@ -143,22 +146,56 @@ __device__ __forceinline__ float logprob(float x, const RowStats &s, float inv_t
   return x == -INFINITY && s.sum == s.sum ? -INFINITY : (x - s.top) * inv_t - LN2 * log2f(s.sum);
 }
 
+// Where the entries of a row are taken from: 2^(x c - ref), one fma and one rounding, and at the largest entry not 1 but 2^off, off = top c - ref, which the
+// finished sums are divided by.  Beyond 2^100 (entries ruled out by the lowest value of a type) neighbouring values lie 2^76 apart: with c = 2^-64 products are
+// exact, and all entries but the largest still vanish.
+struct Anchor { float c, ref; };
+__device__ __forceinline__ Anchor anchor(float top, float c) {
+  if (top == -INFINITY) top = 0.f;
+  if (fabsf(top) > 0x1p100f) c = 0x1p-64f;
+  return {c, top * c};
+}
+__device__ __forceinline__ float anchor_off(float top, const Anchor &a) { return top == -INFINITY ? 0.f : fmaf(top, a.c, -a.ref); }
+
+// Sums of a thread as they grow, relative to the anchor at the largest entry so far.
+struct Running { float top; Anchor at; float sum, turn; };
+__device__ __forceinline__ Running nothing(float c) { return {-INFINITY, {c, 0.f}, 0.f, 0.f}; }
+__device__ __forceinline__ void raise(Running &s, float top, float c) {
+  if (s.top == top) return;
+  const Anchor a = anchor(top, c);
+  // (nothing is left across 2^100, nor was there anything at first)
+  const float d = a.c == s.at.c && s.top != -INFINITY ? fmaxf(s.at.ref - a.ref, -200.f) : -200.f, k = __builtin_amdgcn_exp2f(d);
+  s.turn = fmaf(d, s.sum, s.turn) * k;
+  s.sum *= k;
+  s.top = top; s.at = a;
+}
+// (One entry alone: its sum over itself is 1 and its turn less off times its sum is nought, to the bit, since both products round alike.)
+__device__ __forceinline__ RowStats finished(const Running &s) {
+#pragma clang fp contract(off)
+  const float off = anchor_off(s.top, s.at), e = __builtin_amdgcn_exp2f(off), turned = off * s.sum;
+  return {s.top, s.sum / e, (s.turn - turned) / e};
+}
+
+// The largest entry of a vector.  Halves of either kind compare as whole numbers: the largest signed one if it has no sign, else, all being negative, the least
+// unsigned one; two elements an instruction, and none is widened.  (NaN counts as larger than infinity or is passed over: its term makes the sum NaN.)
 template <int DT> __device__ __forceinline__ float largest(const vec16 &q) {
-  float m = -INFINITY;
+  if constexpr (DT == ECHO_F32) return fmaxf(fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1])), fmaxf(__uint_as_float(q[2]), __uint_as_float(q[3])));
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  const uint32_t w[4] = {q[0], q[1], q[2], q[3]};
+  s16x2 i = __builtin_bit_cast(s16x2, w[0]);
+  u16x2 u = __builtin_bit_cast(u16x2, w[0]);
 #pragma unroll
-  for (int e = 0; e < Elem<DT>::VEC; ++e) m = fmaxf(m, element<DT>(q, e));
-  return m;
-}
-template <int DT> __device__ __forceinline__ void add_entries(RowStats &s, const vec16 &q, float from, float c) {
-#pragma unroll
-  for (int e = 0; e < Elem<DT>::VEC; ++e) {
-    const float d = (element<DT>(q, e) - from) * c, p = __builtin_amdgcn_exp2f(d);
-    s.sum += p;
-    s.turn = fmaf(p, fmaxf(d, -200.f), s.turn);
+  for (int k = 1; k < 4; ++k) {
+    i = __builtin_elementwise_max(i, __builtin_bit_cast(s16x2, w[k]));
+    u = __builtin_elementwise_min(u, __builtin_bit_cast(u16x2, w[k]));
   }
+  const short most = i[0] > i[1] ? i[0] : i[1];
+  const unsigned short least = u[0] < u[1] ? u[0] : u[1];
+  return widen<DT == ECHO_F32 ? ECHO_BF16 : DT>(most >= 0 ? (uint16_t)most : (uint16_t)least);
 }
-// Adds N vectors a thread, vector v of the first thread and those W apart, to a thread's statistics; what does not count (from `end` on, or repeated) becomes -inf.
-template <int DT, int W, int N> __device__ __forceinline__ void add_vectors(RowStats &s, vec16 *q, const Vectors &r, int v, int end, float c, float *of_vector = nullptr) {
+// Adds N vectors a thread, vector v of the first thread and those W apart, to a thread's sums; what does not count (from `end` on, or repeated) becomes -inf.
+template <int DT, int W, int N> __device__ __forceinline__ void add_vectors(Running &s, vec16 *q, const Vectors &r, int v, int end, float c, float *of_vector = nullptr) {
   if (v + N * W > end) {
     const vec16 none = filled<DT>(-INFINITY);
 #pragma unroll
@@ -170,17 +207,20 @@ template <int DT, int W, int N> __device__ __forceinline__ void add_vectors(RowS
   float top = s.top;
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    as_loaded(q[u]);
     const float m = largest<DT>(q[u]);
     if (of_vector) of_vector[u] = m;
     top = fmaxf(top, m);
   }
-  s = moved(s, top, c);
-  const float from = top == -INFINITY ? 0.f : top;
+  raise(s, top, c);
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     as_loaded(q[u]);
-    add_entries<DT>(s, q[u], from, c);
+#pragma unroll
+    for (int e = 0; e < Elem<DT>::VEC; ++e) {
+      const float d = fmaf(element<DT>(q[u], e), s.at.c, -s.at.ref), p = __builtin_amdgcn_exp2f(d);
+      s.sum += p;
+      s.turn = fmaf(p, fmaxf(d, -200.f), s.turn);   // (-inf weighs nothing)
+    }
   }
 }
 
@@ -239,7 +279,7 @@ template <int DT, int BATCH, bool TOP, bool ONE> __global__ __launch_bounds__(TH
   const float c = LOG2E / r.temperature;
   const Vectors row = vectors_of<DT>(r.vocab);
   const int begin = part * span, end = min(row.count, begin + span);   // vectors
-  RowStats s = {-INFINITY, 0.f, 0.f};
+  Running running = nothing(c);
   vec16 q[BATCH];
   float of_vector[BATCH];
 #pragma unroll
@@ -247,10 +287,10 @@ template <int DT, int BATCH, bool TOP, bool ONE> __global__ __launch_bounds__(TH
   for (int v = begin; v < end; v += THREADS * BATCH) {
 #pragma unroll
     for (int u = 0; u < BATCH; ++u) q[u] = load_vector<DT>(x, row, v + u * THREADS + threadIdx.x);
-    add_vectors<DT, THREADS, BATCH>(s, q, row, v, end, c, TOP ? of_vector : nullptr);
+    add_vectors<DT, THREADS, BATCH>(running, q, row, v, end, c, TOP ? of_vector : nullptr);
   }
-  const float mine = s.top;
-  s = block_stats<THREADS / 64>(s, c, sh);
+  const float mine = running.top;
+  const RowStats s = block_stats<THREADS / 64>(finished(running), c, sh);
   if (threadIdx.x == 0) {
     const int given = r.targets ? r.targets[t] : -1, first_entry = entry_of<DT>(row, begin), last_entry = entry_of<DT>(row, end);
     const float logit = given >= first_entry && given < last_entry ? widen<DT>(x[given]) : -INFINITY;
@@ -376,21 +416,24 @@ template <bool TOP> __global__ __launch_bounds__(THREADS) void stats_finish_kern
   }
 }
 
-// Gradient of a row: with d_j = (x_j scale - from) unit and p_j a factor (in a and b) times 2^d_j, out_j = 2^d_j (a + b d_j), at_target more at the
-// target.
-struct RowGrad { float scale, from, unit, a, b, at_target; };
+// Gradient of a row whose p_j are a factor (in a and b) times 2^d_j, d_j = x_j c - ref: out_j = 2^d_j (a + b d_j), at_target more at the target.
+struct RowGrad { float c, ref, a, b, at_target; };
 // Coefficients for d/dlogprob = g and d/dentropy = h, where p_j = k 2^d_j and ln p_j = ln 2 d_j - lo.
-__device__ __forceinline__ RowGrad row_grad(float scale, float from, float unit, float k, float lo, float g, float h, float H, float inv_t) {
-  return {scale, from, unit, -k * inv_t * (g + h * (H - lo)), -k * inv_t * h * LN2, g * inv_t};
+__device__ __forceinline__ RowGrad row_grad(float c, float ref, float k, float lo, float g, float h, float H, float inv_t) {
+  return {c, ref, -k * inv_t * (g + h * (H - lo)), -k * inv_t * h * LN2, g * inv_t};
+}
+// NaN for every entry, also those whose 2^d_j would be 0.
+__device__ __forceinline__ RowGrad nan_grad() { return {0.f, 0.f, NAN, 0.f, 0.f}; }
+// (The product of 0 and an infinity is 0 in v_mul_legacy_f32: an entry of -inf has no gradient.)
+__device__ __forceinline__ float entry_grad(float x, const RowGrad &c) {
+  const float d = fmaf(x, c.c, -c.ref);
+  return mul_legacy(__builtin_amdgcn_exp2f(d), fmaf(c.b, d, c.a));
 }
 template <int DT> __device__ __forceinline__ vec16 grad_vector(const vec16 &q, int from_target, const RowGrad &c) {
   constexpr int VEC = Elem<DT>::VEC;
   float v[VEC];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    const float d = fmaf(element<DT>(q, e), c.scale, -c.from) * c.unit;
-    v[e] = __builtin_amdgcn_exp2f(d) * fmaf(c.b, fmaxf(d, -200.f), c.a);
-  }
+  for (int e = 0; e < VEC; ++e) v[e] = entry_grad(element<DT>(q, e), c);
   if ((uint32_t)from_target < (uint32_t)VEC) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e)
@@ -428,8 +471,11 @@ __device__ __forceinline__ RowGrad finish_loss(const LogitRows &r, const PolicyT
     if (out.logprobs) out.logprobs[t] = l.logprob;
     if (out.entropy) out.entropy[t] = H;
   }
-  if (s.sum == 0.f) return {1.f, 0.f, 1.f, 0.f, 0.f, 0.f};   // without weight anywhere: entries of -inf
-  return row_grad(1.f, s.top, LOG2E / r.temperature, 1.0f / s.sum, LN2 * log2f(s.sum), l.g, l.h, H, inv_t);
+  if (s.sum == 0.f) return {1.f, 0.f, 0.f, 0.f, 0.f};   // without weight anywhere: entries of -inf
+  if (s.sum != s.sum) return nan_grad();
+  const Anchor a = anchor(s.top, LOG2E / r.temperature);
+  const float off = anchor_off(s.top, a);
+  return row_grad(a.c, a.ref, 1.0f / (s.sum * __builtin_amdgcn_exp2f(off)), LN2 * (off + log2f(s.sum)), l.g, l.h, H, inv_t);
 }
 __device__ __forceinline__ void no_loss(const LossOutputs &out, int64_t t) {
   if (out.loss) out.loss[t] = 0.f;
@@ -438,9 +484,14 @@ __device__ __forceinline__ void no_loss(const LossOutputs &out, int64_t t) {
 }
 
 struct GivenStats { const float *lse, *entropy, *g, *h; };   // g, h nullable
+// lse / ln 2 in two parts, the second as a factor of p.  A log-sum beyond 2^100 is that of the largest entries themselves: with c = 2^-64 they have d = 0, or, where
+// x / T was rounded, nearly, and the others vanish.
 __device__ __forceinline__ RowGrad given_grad(const GivenStats &given, int64_t t, float inv_t) {
-  const float h = given.h ? given.h[t] : 0.f;
-  return row_grad(inv_t, given.lse[t], LOG2E, 1.f, 0.f, given.g ? given.g[t] : 0.f, h, given.h ? given.entropy[t] : 0.f, inv_t);
+  const float lse = given.lse[t], h = given.h ? given.h[t] : 0.f, g = given.g ? given.g[t] : 0.f, H = given.h ? given.entropy[t] : 0.f;
+  if (!(lse < INFINITY)) return nan_grad();
+  if (fabsf(lse) > 0x1p100f) return row_grad(0x1p-64f * inv_t, 0x1p-64f * lse, 1.f, 0.f, g, h, H, inv_t);
+  const float hi = lse * LOG2E, lo = fmaf(lse, LOG2E, -hi) + lse * 1.92596299e-8f;
+  return row_grad(LOG2E * inv_t, hi, __builtin_amdgcn_exp2f(-lo), LN2 * lo, g, h, H, inv_t);
 }
 
 // One batch of a row's gradient: from given statistics (LOSS false), or from the parts of stats_kernel, which every workgroup of a row joins while its
@@ -510,18 +561,18 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void l
   vec16 q[N];
 #pragma unroll
   for (int u = 0; u < N; ++u) q[u] = load_vector<DT>(x, row, u * W + threadIdx.x);
-  RowStats s = {-INFINITY, 0.f, 0.f};
+  Running running = nothing(c);
   // a few vectors at a time, as they arrive
 #pragma unroll
-  for (int u = 0; u + AT_ONCE <= N; u += AT_ONCE) add_vectors<DT, W, AT_ONCE>(s, q + u, row, u * W, row.count, c);
-  if constexpr (N % AT_ONCE != 0) add_vectors<DT, W, N % AT_ONCE>(s, q + N / AT_ONCE * AT_ONCE, row, N / AT_ONCE * AT_ONCE * W, row.count, c);
+  for (int u = 0; u + AT_ONCE <= N; u += AT_ONCE) add_vectors<DT, W, AT_ONCE>(running, q + u, row, u * W, row.count, c);
+  if constexpr (N % AT_ONCE != 0) add_vectors<DT, W, N % AT_ONCE>(running, q + N / AT_ONCE * AT_ONCE, row, N / AT_ONCE * AT_ONCE * W, row.count, c);
   for (int v = N * W; v < row.count; v += AGAIN * W) {
     vec16 a[AGAIN];
 #pragma unroll
     for (int u = 0; u < AGAIN; ++u) a[u] = load_vector<DT>(x, row, v + u * W + threadIdx.x);
-    add_vectors<DT, W, AGAIN>(s, a, row, v, row.count, c);
+    add_vectors<DT, W, AGAIN>(running, a, row, v, row.count, c);
   }
-  s = block_stats<W / 64>(s, c, sh);   // (its barrier: the target's logit has been read before any gradient is written)
+  const RowStats s = block_stats<W / 64>(finished(running), c, sh);   // (its barrier: the target's logit has been read before any gradient is written)
   const RowGrad g = finish_loss(r, terms, out, t, s, given, threadIdx.x == 0);
   for (int v = N * W; v < row.count; v += AGAIN * W) {
     vec16 a[AGAIN];
@@ -593,7 +644,7 @@ template <int DT> __global__ __launch_bounds__(THREADS) void narrow_kernel(Logit
     }
     return;
   }
-  RowGrad g = {1.f, 0.f, 1.f, 0.f, 0.f, 0.f};
+  RowGrad g = {1.f, 0.f, 0.f, 0.f, 0.f};
   if (loss) {
     if (live) g = finish_loss(r, terms, out, t, s, logit, true);
     else no_loss(out, t);
@@ -603,8 +654,7 @@ template <int DT> __global__ __launch_bounds__(THREADS) void narrow_kernel(Logit
   auto *o = (typename Elem<DT>::type *)out.grad + t * out.stride;
   for (int j = 0; j < 8; ++j) {
     if (j >= r.vocab) break;
-    const float d = fmaf(v[j], g.scale, -g.from) * g.unit, y = __builtin_amdgcn_exp2f(d) * fmaf(g.b, fmaxf(d, -200.f), g.a) + (j == target ? g.at_target : 0.f);
-    o[j] = narrow<DT>(live ? y : 0.f);
+    o[j] = narrow<DT>(live ? entry_grad(v[j], g) + (j == target ? g.at_target : 0.f) : 0.f);
   }
 }
 
@@ -619,7 +669,8 @@ Split split_of(const LogitRows &x, bool top) {
   const int batch = n > THREADS * MANY && x.rows * ((n + large - 1) / large) < 256 ? FEW : MANY;
   const int whole = THREADS * batch * (top || batch == FEW ? 1 : 4);
   const int splits = (n + whole - 1) / whole;
-  return {splits, (n + splits - 1) / splits, batch};
+  // (whole batches but in the last part: what a batch leaves out is computed all the same)
+  return {splits, splits == 1 ? n : whole, batch};
 }
 size_t parts_bytes(const LogitRows &x, const Split &s) { return s.splits == 1 ? 0 : ((size_t)x.rows * s.splits * sizeof(RowPart) + 255) / 256 * 256; }
 
