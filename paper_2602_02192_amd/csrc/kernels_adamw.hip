@@ -91,29 +91,26 @@ __global__ __launch_bounds__(1024) void norm_finish_kernel(const double *partial
 }
 
 // Four values as E4M3 codes, each the largest code not above value + unit * bits / 2^16, unit the distance of the codes around it (the hardware's conversion,
-// whose random bits are these at its field's top); a magnitude beyond 448, which a rounding of the scale can leave, counts as 448.
+// whose random bits are these at its field's top).
 __device__ __forceinline__ uint32_t e4m3_codes(const float *z, const uint32_t *bits_high) {
-  uint32_t q = 0;
-  float c[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    c[k] = __builtin_amdgcn_fmed3f(z[k], -448.0f, 448.0f);
-    if (z[k] != z[k]) c[k] = z[k];
-  }
-  q = __builtin_amdgcn_cvt_sr_fp8_f32(c[0], bits_high[0], q, 0);
-  q = __builtin_amdgcn_cvt_sr_fp8_f32(c[1], bits_high[1], q, 1);
-  q = __builtin_amdgcn_cvt_sr_fp8_f32(c[2], bits_high[2], q, 2);
-  q = __builtin_amdgcn_cvt_sr_fp8_f32(c[3], bits_high[3], q, 3);
-  return q & (((q & 0x7f7f7f7fu) + 0x7f7f7f7fu) | 0x7f7f7f7fu);   // no sign at a magnitude of 0
+  uint32_t q = __builtin_amdgcn_cvt_sr_fp8_f32(z[0], bits_high[0], 0, 0);
+  q = __builtin_amdgcn_cvt_sr_fp8_f32(z[1], bits_high[1], q, 1);
+  q = __builtin_amdgcn_cvt_sr_fp8_f32(z[2], bits_high[2], q, 2);
+  return __builtin_amdgcn_cvt_sr_fp8_f32(z[3], bits_high[3], q, 3);
 }
+// No sign at a magnitude of 0.
+__device__ __forceinline__ uint32_t without_minus_zero(uint32_t codes) { return codes & (((codes & 0x7f7f7f7fu) + 0x7f7f7f7fu) | 0x7f7f7f7fu); }
+// A magnitude beyond 448, which a rounding of the scale can leave, counts as 448.  NaN stays.
+__device__ __forceinline__ float at_most_448(float z) { return z != z ? z : __builtin_amdgcn_fmed3f(z, -448.0f, 448.0f); }
 __device__ __forceinline__ f32x4 e4m3_values(uint32_t codes, float scale) {
   const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(codes, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(codes, true);
   return f32x4{a[0] * scale, a[1] * scale, b[0] * scale, b[1] * scale};
 }
 
-// A bf16 next to f, by 16 random bits, in the high half; infinities and NaN stay what they are.
-__device__ __forceinline__ uint32_t bf16_by_chance(float f, uint32_t word) {
-  return f != f ? 0x7fc00000u : __float_as_uint(f) + (word & 0xffff);
+// A bf16 next to f, by 16 random bits, in the high half; infinities and NaN stay what they are.  CLEAN: a NaN has no bits set in the low half, as one that comes from a
+// bf16 parameter, so that nothing is carried.
+template <bool CLEAN> __device__ __forceinline__ uint32_t bf16_by_chance(float f, uint32_t word) {
+  return !CLEAN && f != f ? 0x7fc00000u : __float_as_uint(f) + (word & 0xffff);
 }
 
 // Scale of a block whose largest magnitude is `top`, and its reciprocal (0 for a block without weight).
@@ -174,8 +171,8 @@ template <int PT, int GT, int ST, bool WHOLE> __device__ __forceinline__ void st
     load4<PT, WHOLE, int>(P[u], param, b, left);
     load4<GT, WHOLE, int>(G[u], grad, b, left);
     if constexpr (ST == ECHO_F32) {
-      M[u] = *(const f32x4 *)(ms_ + b);
-      V[u] = *(const f32x4 *)(vs_ + b);
+      M[u] = __builtin_nontemporal_load((const f32x4 *)(ms_ + b));
+      V[u] = __builtin_nontemporal_load((const f32x4 *)(vs_ + b));
     } else {
       Mc[u] = *(const uint32_t *)(ms_ + b);
       Vc[u] = *(const uint32_t *)(vs_ + b);
@@ -227,7 +224,11 @@ template <int PT, int GT, int ST, bool WHOLE> __device__ __forceinline__ void st
       }
     } else {
       const u32x4 r = draws(s0 + b, 1, c);
-      const uint32_t q[4] = {bf16_by_chance(p[0], r.x), bf16_by_chance(p[1], r.y), bf16_by_chance(p[2], r.z), bf16_by_chance(p[3], r.w)};
+      uint32_t q[4] = {bf16_by_chance<true>(p[0], r.x), bf16_by_chance<true>(p[1], r.y), bf16_by_chance<true>(p[2], r.z), bf16_by_chance<true>(p[3], r.w)};
+      if (!moderate) {
+        q[0] = bf16_by_chance<false>(p[0], r.x); q[1] = bf16_by_chance<false>(p[1], r.y);
+        q[2] = bf16_by_chance<false>(p[2], r.z); q[3] = bf16_by_chance<false>(p[3], r.w);
+      }
       const uint32_t pairs[2] = {__builtin_amdgcn_perm(q[1], q[0], 0x07060302u), __builtin_amdgcn_perm(q[3], q[2], 0x07060302u)};
       uint16_t w[4];
       __builtin_memcpy(w, pairs, 8);
@@ -256,23 +257,30 @@ template <int PT, int GT, int ST, bool WHOLE> __device__ __forceinline__ void st
       const u32x4 r = draws(s0 + b, 0, c);
       const uint32_t low[4] = {r.x << 16, r.y << 16, r.z << 16, r.w << 16}, high[4] = {r.x & 0xffff0000u, r.y & 0xffff0000u, r.z & 0xffff0000u, r.w & 0xffff0000u};
       const float mi = of_lane(inv, 2 * u), vi = of_lane(inv, 2 * u + 1);
-      float z[4];
+      // A positive v of less than the least code has that code whatever the bits.
+      float zm[4], zv[4];
+      if (moderate) {   // all of them are numbers and none is 0
 #pragma unroll
-      for (int k = 0; k < 4; ++k) z[k] = M[u][k] * mi;
-      *(uint32_t *)(ms_ + b) = e4m3_codes(z, low);
-      // a positive v at the least code's value has that code whatever the bits
-      const float least = vi > 0.f ? 0x1p-9f : 0.f;
+        for (int k = 0; k < 4; ++k) {
+          zm[k] = __builtin_amdgcn_fmed3f(M[u][k] * mi, -448.0f, 448.0f);
+          zv[k] = __builtin_amdgcn_fmed3f(V[u][k] * vi, 0x1p-9f, 448.0f);
+        }
+      } else {
+        const float least = vi > 0.f ? 0x1p-9f : 0.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        z[k] = V[u][k] * vi;
-        if (V[u][k] > 0.f && z[k] < least) z[k] = least;
+        for (int k = 0; k < 4; ++k) {
+          zm[k] = at_most_448(M[u][k] * mi);
+          zv[k] = at_most_448(V[u][k] * vi);
+          if (V[u][k] > 0.f && zv[k] < least) zv[k] = least;
+        }
       }
-      *(uint32_t *)(vs_ + b) = e4m3_codes(z, high);
+      *(uint32_t *)(ms_ + b) = without_minus_zero(e4m3_codes(zm, low));
+      *(uint32_t *)(vs_ + b) = e4m3_codes(zv, high);
     }
   }
 }
 
-template <int PT, int GT, int ST> __global__ __launch_bounds__(THREADS) void adamw_kernel(StepTensors t, StepConstants c) {
+template <int PT, int GT, int ST> __global__ __launch_bounds__(THREADS, 6) void adamw_kernel(StepTensors t, StepConstants c) {
   float factor = 1.0f;
   if (c.norm) {
     const float norm = *c.norm;

@@ -6,8 +6,9 @@
 
 namespace echo {
 
-// Magnitudes from 2^-90 to below 2^90: nothing below leaves the normal numbers.  0 is not among them.
-constexpr uint32_t MODERATE_LOW = (uint32_t)(127 - 90) << 24, MODERATE_SPAN = (uint32_t)180 << 24;
+// Magnitudes from 2^-80 to below 2^80: nothing below leaves the normal numbers, nor does a quotient by something as small as the root of the least.  0 is not
+// among them.
+constexpr uint32_t MODERATE_LOW = (uint32_t)(127 - 80) << 24, MODERATE_SPAN = (uint32_t)160 << 24;
 // How far a magnitude lies beyond the least moderate one; as a whole number without sign, at least MODERATE_SPAN for all that are not moderate.
 __device__ __forceinline__ uint32_t beyond_moderate(float x) { return (__float_as_uint(x) << 1) - MODERATE_LOW; }
 

@@ -191,6 +191,20 @@ def test_gradients_that_are_not_finite_without_a_norm(learner):
         assert torch.isfinite(p[0][:3]).all() and torch.isnan(opt.m.float()[3])
 
 
+def test_bf16_parameters_that_are_not_finite_stay_so(learner):
+    for states in (torch.float32, torch.float8_e4m3fn):
+        p, g, _ = problem([1000], 4, "bf16", "bf16")
+        g[0][:].add_(1e-3)
+        bad = {3: float("nan"), 4: float("inf"), 700: float("-inf"), 999: float("nan")}
+        for i, v in bad.items():
+            p[0][i] = v
+        opt = learner.AdamW(p, lr=1e-3, weight_decay=0.1, state_dtype=states)
+        for _ in range(3):
+            opt.step(g)
+        assert torch.isnan(p[0][[3, 999]]).all() and p[0][4] == float("inf") and p[0][700] == float("-inf")
+        assert torch.isfinite(p[0][[i for i in range(1000) if i not in bad]]).all()
+
+
 def test_zero_gradients_and_tiny_ones(learner):
     for states in (torch.float32, torch.float8_e4m3fn):
         p = [torch.ones(600, device="cuda")]
@@ -229,6 +243,23 @@ def test_averages_of_every_size(learner, scale):
         want = plain.adamw(np.ones(n, np.float32), gn, np.zeros(n, np.float32), np.zeros(n, np.float32), 0.0, step=1, factor=1.0, **hyper)
         for got, ref in zip((p[0], m[:n], v[:n]), want):
             assert np.array_equal(host(got), ref)
+
+
+def test_states_far_apart(learner):
+    """Averages that do not go together, as a damaged checkpoint has them: large m over the root of a small v passes the end of f32."""
+    n = 1024
+    r = np.random.default_rng(3)
+    m0 = np.ldexp(r.normal(0, 1, n), r.integers(-100, 100, n)).astype(np.float32)
+    v0 = np.ldexp(np.abs(r.normal(0, 1, n)), r.integers(-100, 100, n)).astype(np.float32)
+    m0[256:512], v0[256:512] = np.ldexp(m0[256:512], 0) * 0 + 2.0 ** 79, 2.0 ** -79
+    for eps in (1e-8, 2.0 ** -60):
+        p, g = [torch.ones(n, device="cuda")], [torch.zeros(n, device="cuda")]
+        m, v = torch.from_numpy(m0).cuda(), torch.from_numpy(v0).cuda()
+        hyper = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=eps)
+        learner.adamw_step(p, g, m, v, step=100000, **hyper)
+        want = plain.adamw(np.ones(n, np.float32), np.zeros(n, np.float32), m0, v0, 0.0, step=100000, factor=1.0, **hyper)
+        for got, ref in zip((p[0], m, v), want):
+            assert np.array_equal(host(got), ref, equal_nan=True)
 
 
 def test_state_dict_and_graph(learner):
