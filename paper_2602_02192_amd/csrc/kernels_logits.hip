@@ -552,6 +552,7 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void l
   const Vectors row = vectors_of<DT>(r.vocab);
   if (!token_live(r, terms, t)) {
     if (threadIdx.x == 0) no_loss(out, t);
+    if (!out.grad) return;
     for (int v = threadIdx.x; v < row.count; v += W) store_vector<DT, true>(o, row, v, vec16{0, 0, 0, 0});
     return;
   }
@@ -574,6 +575,7 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void l
   }
   const RowStats s = block_stats<W / 64>(finished(running), c, sh);   // (its barrier: the target's logit has been read before any gradient is written)
   const RowGrad g = finish_loss(r, terms, out, t, s, given, threadIdx.x == 0);
+  if (!out.grad) return;
   for (int v = N * W; v < row.count; v += AGAIN * W) {
     vec16 a[AGAIN];
 #pragma unroll
@@ -684,11 +686,7 @@ size_t logprobs_workspace(const LogitRows &x, int top_k) {
 // Whether a workgroup takes a row whole, or several take parts of it and its gradient in two launches.  Short rows whole in any number; long ones where there are
 // enough to fill the GPU.  151936 entries, bf16: 64 rows 30 us whole, 20 in parts; 128 rows 31 and 31; 200 rows 33 and 41.  f32: 29 and 23, 36 and 40, 50 and 73.
 static bool by_rows(const LogitRows &x) { return row_vectors(x) <= 8192 || x.rows >= 128; }
-size_t policy_workspace(const LogitRows &x) {
-  // (without a gradient the loss is found from the parts)
-  const Split s = split_of(x, false);
-  return ((size_t)x.rows * s.splits * sizeof(RowPart) + 255) / 256 * 256;
-}
+size_t policy_workspace(const LogitRows &x) { return by_rows(x) ? 0 : parts_bytes(x, split_of(x, false)); }
 
 #define FOR_DTYPE(dt, CALL)                                    \
   do {                                                         \
@@ -736,7 +734,7 @@ void launch_policy_loss(const LogitRows &x, const PolicyTerms &terms, float *los
   const Parts p = {(RowPart *)workspace, nullptr};
   const LossOutputs o = {loss, logprobs, entropy, grad, grad_stride};
   if (is_narrow(x)) return launch_narrow(x, st, false, RowOutputs{}, true, GivenStats{}, terms, o);
-  if (grad && by_rows(x)) {
+  if (by_rows(x)) {
     const dim3 grid((uint32_t)x.rows);
     // Registers for short rows; two workgroups a CU, one of which waits for memory while the other computes, for long ones, of which they hold a part.  2048 rows of
     // 9000 bf16: 24 us by 256 threads, 41 by 512; of 32000: 52 and 50, 86 with room for 18 vectors; of 151936: 298 by one workgroup a CU that holds the row, 264 by
