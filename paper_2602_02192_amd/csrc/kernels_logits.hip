@@ -194,32 +194,40 @@ template <int DT> __device__ __forceinline__ float largest(const vec16 &q) {
   const unsigned short least = u[0] < u[1] ? u[0] : u[1];
   return widen<DT == ECHO_F32 ? ECHO_BF16 : DT>(most >= 0 ? (uint16_t)most : (uint16_t)least);
 }
-// Adds N vectors a thread, vector v of the first thread and those W apart, to a thread's sums; what does not count (from `end` on, or repeated) becomes -inf.
+// Adds N vectors a thread, vector v of the first thread and those W apart, to a thread's sums; what does not count (from `end` on, or repeated) becomes -inf.  A few
+// at a time: those that lie beyond `end` altogether cost nothing.
+constexpr int AT_ONCE = 4;
 template <int DT, int W, int N> __device__ __forceinline__ void add_vectors(Running &s, vec16 *q, const Vectors &r, int v, int end, float c, float *of_vector = nullptr) {
-  if (v + N * W > end) {
-    const vec16 none = filled<DT>(-INFINITY);
+  if constexpr (N > AT_ONCE) {
+    add_vectors<DT, W, AT_ONCE>(s, q, r, v, end, c, of_vector);
+    add_vectors<DT, W, N - AT_ONCE>(s, q + AT_ONCE, r, v + AT_ONCE * W, end, c, of_vector ? of_vector + AT_ONCE : nullptr);
+  } else {
+    if (v >= end) return;
+    if (v + N * W > end) {
+      const vec16 none = filled<DT>(-INFINITY);
 #pragma unroll
-    for (int u = 0; u < N; ++u)
+      for (int u = 0; u < N; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) q[u][i] = v + u * W + (int)threadIdx.x < end ? q[u][i] : none[i];
-  }
-  if (v == 0 && r.repeated && threadIdx.x == 0) q[0] = own_entries<DT>(q[0], r.repeated);
-  float top = s.top;
+        for (int i = 0; i < 4; ++i) q[u][i] = v + u * W + (int)threadIdx.x < end ? q[u][i] : none[i];
+    }
+    if (v == 0 && r.repeated && threadIdx.x == 0) q[0] = own_entries<DT>(q[0], r.repeated);
+    float top = s.top;
 #pragma unroll
-  for (int u = 0; u < N; ++u) {
-    const float m = largest<DT>(q[u]);
-    if (of_vector) of_vector[u] = m;
-    top = fmaxf(top, m);
-  }
-  raise(s, top, c);
+    for (int u = 0; u < N; ++u) {
+      const float m = largest<DT>(q[u]);
+      if (of_vector) of_vector[u] = m;
+      top = fmaxf(top, m);
+    }
+    raise(s, top, c);
 #pragma unroll
-  for (int u = 0; u < N; ++u) {
-    as_loaded(q[u]);
+    for (int u = 0; u < N; ++u) {
+      as_loaded(q[u]);
 #pragma unroll
-    for (int e = 0; e < Elem<DT>::VEC; ++e) {
-      const float d = fmaf(element<DT>(q[u], e), s.at.c, -s.at.ref), p = __builtin_amdgcn_exp2f(d);
-      s.sum += p;
-      s.turn = fmaf(p, fmaxf(d, -200.f), s.turn);   // (-inf weighs nothing)
+      for (int e = 0; e < Elem<DT>::VEC; ++e) {
+        const float d = fmaf(element<DT>(q[u], e), s.at.c, -s.at.ref), p = __builtin_amdgcn_exp2f(d);
+        s.sum += p;
+        s.turn = fmaf(p, fmaxf(d, -200.f), s.turn);   // (-inf weighs nothing)
+      }
     }
   }
 }
@@ -544,7 +552,7 @@ template <int DT, bool LOSS> __global__ __launch_bounds__(THREADS) void grad_ker
 // A whole row by one workgroup: its first N vectors a thread stay in registers between the statistics and the gradient, what is beyond them is read
 // again.
 template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void loss_row_kernel(LogitRows r, PolicyTerms terms, LossOutputs out) {
-  constexpr int AGAIN = 4, AT_ONCE = 4;
+  constexpr int AGAIN = 4;
   __shared__ RowStats sh[W / 64];
   const int64_t t = blockIdx.x;
   const auto *x = (const typename Elem<DT>::type *)r.x + t * r.stride;
@@ -563,20 +571,22 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void l
 #pragma unroll
   for (int u = 0; u < N; ++u) q[u] = load_vector<DT>(x, row, u * W + threadIdx.x);
   Running running = nothing(c);
-  // a few vectors at a time, as they arrive
-#pragma unroll
-  for (int u = 0; u + AT_ONCE <= N; u += AT_ONCE) add_vectors<DT, W, AT_ONCE>(running, q + u, row, u * W, row.count, c);
-  if constexpr (N % AT_ONCE != 0) add_vectors<DT, W, N % AT_ONCE>(running, q + N / AT_ONCE * AT_ONCE, row, N / AT_ONCE * AT_ONCE * W, row.count, c);
-  for (int v = N * W; v < row.count; v += AGAIN * W) {
+  add_vectors<DT, W, N>(running, q, row, 0, row.count, c);   // (as they arrive)
+  int v = N * W;
+  for (; v + AGAIN * W <= row.count; v += AGAIN * W) {
     vec16 a[AGAIN];
 #pragma unroll
     for (int u = 0; u < AGAIN; ++u) a[u] = load_vector<DT>(x, row, v + u * W + threadIdx.x);
     add_vectors<DT, W, AGAIN>(running, a, row, v, row.count, c);
   }
+  for (; v < row.count; v += W) {
+    vec16 a = load_vector<DT>(x, row, v + threadIdx.x);
+    add_vectors<DT, W, 1>(running, &a, row, v, row.count, c);
+  }
   const RowStats s = block_stats<W / 64>(finished(running), c, sh);   // (its barrier: the target's logit has been read before any gradient is written)
   const RowGrad g = finish_loss(r, terms, out, t, s, given, threadIdx.x == 0);
   if (!out.grad) return;
-  for (int v = N * W; v < row.count; v += AGAIN * W) {
+  for (v = N * W; v + AGAIN * W <= row.count; v += AGAIN * W) {
     vec16 a[AGAIN];
 #pragma unroll
     for (int u = 0; u < AGAIN; ++u) a[u] = load_vector<DT>(x, row, v + u * W + threadIdx.x);
@@ -586,6 +596,10 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void l
       as_loaded(a[u]);
       store_vector<DT, true>(o, row, w, grad_vector<DT>(a[u], target - entry_of<DT>(row, w), g));
     }
+  }
+  for (; v < row.count; v += W) {
+    const int w = v + threadIdx.x;
+    store_vector<DT, true>(o, row, w, grad_vector<DT>(load_vector<DT>(x, row, w), target - entry_of<DT>(row, w), g));
   }
 #pragma unroll
   for (int u = 0; u < N; ++u) {
@@ -660,19 +674,19 @@ template <int DT> __global__ __launch_bounds__(THREADS) void narrow_kernel(Logit
   }
 }
 
-// Parts of a row: one batch each where the top entries are wanted, a few batches otherwise; of few rows small batches, so that there are parts for the
-// whole GPU.
+// Parts of a row: one batch each where the top entries are wanted, up to four otherwise, as many as leave some thousand parts; of few rows small batches, so that there
+// are parts for the whole GPU.
 struct Split { int splits, span, batch; };   // span: vectors of a part
 int vector_entries(const LogitRows &x) { return x.dtype == ECHO_F32 ? 4 : 8; }
 int row_vectors(const LogitRows &x) { return (x.vocab + vector_entries(x) - 1) / vector_entries(x); }
 bool is_narrow(const LogitRows &x) { return x.vocab < vector_entries(x); }
 Split split_of(const LogitRows &x, bool top) {
-  const int n = row_vectors(x), large = THREADS * MANY * (top ? 1 : 4);
-  const int batch = n > THREADS * MANY && x.rows * ((n + large - 1) / large) < 256 ? FEW : MANY;
-  const int whole = THREADS * batch * (top || batch == FEW ? 1 : 4);
-  const int splits = (n + whole - 1) / whole;
-  // (whole batches but in the last part: what a batch leaves out is computed all the same)
-  return {splits, splits == 1 ? n : whole, batch};
+  const int n = row_vectors(x), large = (n + THREADS * MANY - 1) / (THREADS * MANY);   // large batches
+  if (large == 1 || (!top && large <= 4)) return {1, n, MANY};   // (one launch: 1024 rows of 34000 bf16 19 us, 23 in parts)
+  if (x.rows * large < 256) return {(n + THREADS * FEW - 1) / (THREADS * FEW), THREADS * FEW, FEW};
+  const int64_t wanted = top ? 1 : x.rows * large / 4096;
+  const int most = wanted < 1 ? 1 : wanted < 4 ? (int)wanted : 4, splits = (large + most - 1) / most, each = (large + splits - 1) / splits;
+  return {(large + each - 1) / each, each * THREADS * MANY, MANY};
 }
 size_t parts_bytes(const LogitRows &x, const Split &s) { return s.splits == 1 ? 0 : ((size_t)x.rows * s.splits * sizeof(RowPart) + 255) / 256 * 256; }
 
