@@ -59,21 +59,44 @@ template <int WAVES> __device__ double block_sum(double v, double *sh) {
   return v;
 }
 
-// A square of f32 is exact in f64, so the sum loses next to nothing and does not depend on sizes or order to within its rounding to f32.
+// Sum of the squares of 16 bytes of gradient.  A square of f32 is exact in f64, so the sum loses next to nothing and does not depend on sizes or order to within its
+// rounding to f32.
+template <int DT> __device__ __forceinline__ void add_squares(double *s, const uint32_t *q) {
+  constexpr int VEC = DT == ECHO_F32 ? 4 : 8;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    float g;
+    if constexpr (DT == ECHO_F32) g = __uint_as_float(q[e]);
+    else if constexpr (DT == ECHO_BF16) g = __uint_as_float(e % 2 ? q[e / 2] & 0xffff0000u : q[e / 2] << 16);
+    else g = h16_bits_to_f32((uint16_t)(e % 2 ? q[e / 2] >> 16 : q[e / 2]));
+    s[e % 4] = fma((double)g, (double)g, s[e % 4]);
+  }
+}
 template <int DT> __global__ __launch_bounds__(THREADS) void norm_kernel(NormTensors t, double *partial) {
   __shared__ double sh[THREADS / 64];
-  constexpr int N = 8;
+  typedef typename std::conditional<DT == ECHO_F32, uint32_t, uint16_t>::type Bits;
+  constexpr int VEC = 16 / sizeof(Bits), N = 8192 / (THREADS * VEC);
   const int i = tensor_of(t.chunk0, t.n, blockIdx.x);
   const int64_t a = (int64_t)(blockIdx.x - t.chunk0[i]) * t.chunk, end = min(t.numel[i], a + t.chunk);
+  const Bits *g = (const Bits *)t.grad[i];
   double s[4] = {0, 0, 0, 0};
-  for (int64_t b = a; b < end; b += THREADS * 4 * N) {
-    f32x4 g[N];
+  int64_t b = a;
+  for (; b + 8192 <= end; b += 8192) {
+    uint32_t q[N][4];
 #pragma unroll
-    for (int u = 0; u < N; ++u) load4<DT>(g[u], t.grad[i], b + (u * THREADS + (int)threadIdx.x) * 4, end);
+    for (int u = 0; u < N; ++u) __builtin_memcpy(q[u], g + b + (u * THREADS + threadIdx.x) * VEC, 16);
 #pragma unroll
-    for (int u = 0; u < N; ++u)
+    for (int u = 0; u < N; ++u) add_squares<DT>(s, q[u]);
+  }
+  for (b += threadIdx.x * VEC; b < end; b += THREADS * VEC) {
+    Bits e[VEC];
+    if (b + VEC <= end) __builtin_memcpy(e, g + b, 16);
+    else
 #pragma unroll
-      for (int k = 0; k < 4; ++k) s[k] = fma((double)g[u][k], (double)g[u][k], s[k]);
+      for (int k = 0; k < VEC; ++k) e[k] = b + k < end ? g[b + k] : (Bits)0;
+    uint32_t q[4];
+    __builtin_memcpy(q, e, 16);
+    add_squares<DT>(s, q);
   }
   const double all = block_sum<THREADS / 64>(s[0] + s[1] + s[2] + s[3], sh);
   if (threadIdx.x == 0) partial[blockIdx.x] = all;
