@@ -147,12 +147,14 @@ __device__ __forceinline__ float logprob(float x, const RowStats &s, float inv_t
 }
 
 // Where the entries of a row are taken from: 2^(x c - ref), one fma and one rounding, and at the largest entry not 1 but 2^off, off = top c - ref, which the
-// finished sums are divided by.  Beyond 2^100 (entries ruled out by the lowest value of a type) neighbouring values lie 2^76 apart: with c = 2^-64 products are
-// exact, and all entries but the largest still vanish.
+// finished sums are divided by.  Where ref would pass 2^29 (rows in which everything is ruled out by a large negative number), neighbouring values are a factor of 2^32
+// apart and more: a power of two that puts the top beyond 2^29 is a c as good, with exact products, and all entries but the largest vanish.
 struct Anchor { float c, ref; };
 __device__ __forceinline__ Anchor anchor(float top, float c) {
   if (top == -INFINITY) top = 0.f;
-  if (fabsf(top) > 0x1p100f) c = 0x1p-64f;
+  const float ref = top * c;
+  if (!(fabsf(ref) > 0x1p29f)) return {c, ref};
+  c = __builtin_amdgcn_ldexpf(1.0f, min(127, 31 - __builtin_amdgcn_frexp_expf(top)));
   return {c, top * c};
 }
 __device__ __forceinline__ float anchor_off(float top, const Anchor &a) { return top == -INFINITY ? 0.f : fmaf(top, a.c, -a.ref); }
@@ -163,7 +165,7 @@ __device__ __forceinline__ Running nothing(float c) { return {-INFINITY, {c, 0.f
 __device__ __forceinline__ void raise(Running &s, float top, float c) {
   if (s.top == top) return;
   const Anchor a = anchor(top, c);
-  // (nothing is left across 2^100, nor was there anything at first)
+  // (between different c nothing is left, nor was there anything at first)
   const float d = a.c == s.at.c && s.top != -INFINITY ? fmaxf(s.at.ref - a.ref, -200.f) : -200.f, k = __builtin_amdgcn_exp2f(d);
   s.turn = fmaf(d, s.sum, s.turn) * k;
   s.sum *= k;
@@ -437,17 +439,21 @@ __device__ __forceinline__ float entry_grad(float x, const RowGrad &c) {
   const float d = fmaf(x, c.c, -c.ref);
   return mul_legacy(__builtin_amdgcn_exp2f(d), fmaf(c.b, d, c.a));
 }
-template <int DT> __device__ __forceinline__ vec16 grad_vector(const vec16 &q, int from_target, const RowGrad &c) {
+template <int DT, typename F> __device__ __forceinline__ vec16 grad_vector(const vec16 &q, int from_target, const RowGrad &c, F entry) {
   constexpr int VEC = Elem<DT>::VEC;
   float v[VEC];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) v[e] = entry_grad(element<DT>(q, e), c);
+  for (int e = 0; e < VEC; ++e) v[e] = entry(element<DT>(q, e), c);
   if ((uint32_t)from_target < (uint32_t)VEC) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e)
       if (e == from_target) v[e] += c.at_target;
   }
   return pack<DT>(v);
+}
+
+template <int DT> __device__ __forceinline__ vec16 grad_vector(const vec16 &q, int from_target, const RowGrad &c) {
+  return grad_vector<DT>(q, from_target, c, [](float x, const RowGrad &g) { return entry_grad(x, g); });
 }
 
 struct TokenLoss { float loss, logprob, g, h; };
@@ -458,7 +464,7 @@ __device__ TokenLoss token_loss(const PolicyTerms &p, int64_t t, float lp, float
   float kl = 0.f, kl_slope = 0.f;
   if (p.kl != 0.f) {
     const float off = p.ref[t] - lp, e = expm1f(off);
-    kl = p.kl * (e - off);
+    kl = p.kl * (e == INFINITY ? e : e - off);
     kl_slope = -p.kl * e;
   }
   const float slope = free <= held && ratio < p.ratio_cap ? A * ratio : 0.f;
@@ -492,14 +498,21 @@ __device__ __forceinline__ void no_loss(const LossOutputs &out, int64_t t) {
 }
 
 struct GivenStats { const float *lse, *entropy, *g, *h; };   // g, h nullable
-// lse / ln 2 in two parts, the second as a factor of p.  A log-sum beyond 2^100 is that of the largest entries themselves: with c = 2^-64 they have d = 0, or, where
-// x / T was rounded, nearly, and the others vanish.
+// A log-sum beyond this is, to its own rounding, the largest entry itself.
+constexpr float FAR_LSE = 0x1p28f;
+// lse / ln 2 in two parts, the second as a factor of p.
 __device__ __forceinline__ RowGrad given_grad(const GivenStats &given, int64_t t, float inv_t) {
   const float lse = given.lse[t], h = given.h ? given.h[t] : 0.f, g = given.g ? given.g[t] : 0.f, H = given.h ? given.entropy[t] : 0.f;
   if (!(lse < INFINITY)) return nan_grad();
-  if (fabsf(lse) > 0x1p100f) return row_grad(0x1p-64f * inv_t, 0x1p-64f * lse, 1.f, 0.f, g, h, H, inv_t);
+  if (fabsf(lse) > FAR_LSE) return row_grad(inv_t, lse, 1.f, 0.f, g, h, H, inv_t);
   const float hi = lse * LOG2E, lo = fmaf(lse, LOG2E, -hi) + lse * 1.92596299e-8f;
   return row_grad(LOG2E * inv_t, hi, __builtin_amdgcn_exp2f(-lo), LN2 * lo, g, h, H, inv_t);
+}
+// An entry of a row with such a log-sum (c: 1 / T, ref: lse): x / T is rounded as lse was, so the largest entries have d = 0.
+__device__ __forceinline__ float far_entry_grad(float x, const RowGrad &c) {
+#pragma clang fp contract(off)
+  const float y = x * c.c, d = fminf((y - c.ref) * LOG2E, 0.f);
+  return mul_legacy(__builtin_amdgcn_exp2f(d), fmaf(c.b, d, c.a));
 }
 
 // One batch of a row's gradient: from given statistics (LOSS false), or from the parts of stats_kernel, which every workgroup of a row joins while its
@@ -540,6 +553,14 @@ template <int DT, bool LOSS> __global__ __launch_bounds__(THREADS) void grad_ker
   } else {
     c = given_grad(given, t, 1.0f / r.temperature);
     if (given.g) target = r.targets[t];
+    if (fabsf(given.lse[t]) > FAR_LSE) {
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const int v = begin + u * THREADS + threadIdx.x;
+        store_vector<DT>(o, row, v, grad_vector<DT>(q[u], target - entry_of<DT>(row, v), c, [](float x, const RowGrad &g) { return far_entry_grad(x, g); }));
+      }
+      return;
+    }
   }
 #pragma unroll
   for (int u = 0; u < BATCH; ++u) {
@@ -670,7 +691,8 @@ template <int DT> __global__ __launch_bounds__(THREADS) void narrow_kernel(Logit
   auto *o = (typename Elem<DT>::type *)out.grad + t * out.stride;
   for (int j = 0; j < 8; ++j) {
     if (j >= r.vocab) break;
-    o[j] = narrow<DT>(live ? entry_grad(v[j], g) + (j == target ? g.at_target : 0.f) : 0.f);
+    const bool far = !loss && live && fabsf(given.lse[t]) > FAR_LSE;
+    o[j] = narrow<DT>(live ? (far ? far_entry_grad(v[j], g) : entry_grad(v[j], g)) + (j == target ? g.at_target : 0.f) : 0.f);
   }
 }
 

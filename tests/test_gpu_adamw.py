@@ -296,6 +296,23 @@ def test_state_dict_and_graph(learner):
         assert all(torch.equal(a, b) for a, b in zip(p, q)) and torch.equal(state[0], state[2])
 
 
+def test_tensors_beyond_32_bits_of_elements(learner):
+    n = 2 ** 31 + 5000                               # the parameter's end lies beyond 2^32 bytes, the last elements beyond 2^31
+    p, g = [torch.full((1000,), 0.5, dtype=torch.bfloat16, device="cuda"), torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda")], []
+    g = [torch.ones(1000, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")]
+    g[1][-4000:] = 2.0
+    g[1][:300] = 1.0
+    norm = learner.grad_norm(g)
+    assert abs(float(norm) / np.sqrt(1300 + 4 * 4000) - 1) < 2e-7
+    opt = learner.AdamW(p, lr=0.125, state_dtype=torch.float8_e4m3fn, seed=5)
+    opt.step(g)
+    # the first step moves by lr against the gradient's sign: 0.375 is a bf16, and next to it what rounding by chance gives
+    assert ((p[1][-4000:].float() - 0.375).abs() < 0.004).all() and ((p[1][:300].float() - 0.375).abs() < 0.004).all()
+    assert (p[1][300:1000] == 0.5).all() and (p[1][2 ** 31 - 3000:2 ** 31 + 500] == 0.5).all()
+    at = n // 256 * 256 + 1024
+    assert (opt.m[1024 + n - 4000:1024 + n].float() > 0).all() and (opt.m[1024 + n:].float() == 0).all() and at > 0
+
+
 def test_refusals(learner):
     from paper_2602_02192_amd.echo import EchoError
     p, g = [torch.zeros(300, device="cuda")], [torch.zeros(300, device="cuda")]

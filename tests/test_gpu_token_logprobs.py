@@ -211,6 +211,41 @@ def test_gradient_against_differences(learner):
     check_grad(only.grad, x, want, targets.cpu().numpy(), np.ones(2), np.zeros(2), T, "f32")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [5, 1000, 40003, 151936])
+def test_rows_in_which_everything_is_ruled_out_by_a_large_number(learner, dtype, vocab):
+    """Equal entries of any size are a uniform distribution; beside an ordinary entry they have no weight."""
+    values = [-1e4, -6.1e5, -1e9, -1.3e9, -1e10, -1e15, -3e20, 1e10, 7e25, 3e38, -3e38]
+    x = torch.tensor(values, device="cuda")[:, None].expand(-1, vocab).to(DT[dtype]).contiguous()
+    rows = len(values)
+    targets = torch.full((rows,), vocab - 1, dtype=torch.int32, device="cuda")
+    one, loss = torch.ones(rows, device="cuda"), dict(clip_low=0.2, clip_high=0.2, kl_coef=0.0, entropy_coef=0.1)
+    for T in (1.0, 1.25):
+        got = learner.token_logprobs(x, targets, temperature=T, top_k=3)
+        for v in (got.logprobs, got.top_logprobs[:, 0], got.top_logprobs[:, 2], -got.entropy):
+            np.testing.assert_allclose(f64(v), -np.log(vocab), atol=1e-5)
+        assert (got.top_ids == torch.arange(3, device="cuda")).all()
+        out = learner.policy_loss(x, targets, one, got.logprobs, temperature=T, **loss)
+        # ratio 1: d loss / d x_j = -(1[j = target] - p) / T, entropy at its largest
+        np.testing.assert_allclose(f64(out.logprobs), -np.log(vocab), atol=1e-5)
+        want = np.full(vocab, 1 / vocab) / T
+        want[-1] -= 1 / T
+        np.testing.assert_allclose(f64(out.grad_logits), np.broadcast_to(want, (rows, vocab)), rtol=ROUND[dtype] + 1e-4, atol=1e-6 / vocab)
+        grad = learner.token_logprobs_grad(x, targets, got.lse, got.entropy, one, one, temperature=T)
+        assert torch.isfinite(grad).all() and (grad.float().abs() <= 2 * (1 + np.log(vocab)) / T).all()
+    x[:, 1] = torch.where(x[:, 1] < 0, 2.0, x[:, 1].float()).to(x.dtype)
+    got = learner.token_logprobs(x, targets.clamp(max=0) + 1)
+    below = [i for i, v in enumerate(values) if v < 0]
+    assert (got.logprobs[below] == 0).all() and (got.entropy[below] == 0).all() and (got.lse[below] == 2.0).all()
+
+
+def test_temperatures_of_every_size(learner):
+    x, targets, _ = make(6, 3001, "f32", 91)
+    for T in (1e-6, 1e-3, 50.0, 1e6, 1e30):
+        check(learner, x, targets, T, 4)
+        check(learner, x * T, targets, T, 4)
+
+
 def test_same_bits_again_and_on_another_stream(learner):
     x, targets, _ = make(130, 40007, "bf16", 2)
     a = learner.token_logprobs(x, targets, top_k=9)
