@@ -67,8 +67,8 @@ template <int DT> __device__ __forceinline__ vec16 load_vector(const typename El
   __builtin_memcpy(&q, (const char *)x + byte_of<DT>(entry_of<DT>(r, min(v, r.count - 1))), 16);
   return q;
 }
-// ONCE: past the caches, which keep what is read again.
-template <int DT, bool ONCE = false> __device__ __forceinline__ void store_vector(typename Elem<DT>::type *x, const Vectors &r, int v, const vec16 &q) {
+// (Past the caches, which keep what is read again: 777 rows of 32001 f32 37 -> 28 us, 512 of 151936 bf16 62 -> 59.)
+template <int DT> __device__ __forceinline__ void store_vector(typename Elem<DT>::type *x, const Vectors &r, int v, const vec16 &q) {
   if (v == 0 && r.repeated) {
     typename Elem<DT>::type e[Elem<DT>::VEC];
     __builtin_memcpy(e, &q, 16);
@@ -78,7 +78,7 @@ template <int DT, bool ONCE = false> __device__ __forceinline__ void store_vecto
   } else if (v < r.count) {
     typedef vec16 __attribute__((aligned(2))) vec;
     vec *to = (vec *)((char *)x + byte_of<DT>(entry_of<DT>(r, v)));
-    if (ONCE) __builtin_nontemporal_store(q, to); else *to = q;
+    __builtin_nontemporal_store(q, to);
   }
 }
 // Vector 0 with -inf in place of the entries it repeats.
@@ -582,7 +582,7 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void l
   if (!token_live(r, terms, t)) {
     if (threadIdx.x == 0) no_loss(out, t);
     if (!out.grad) return;
-    for (int v = threadIdx.x; v < row.count; v += W) store_vector<DT, true>(o, row, v, vec16{0, 0, 0, 0});
+    for (int v = threadIdx.x; v < row.count; v += W) store_vector<DT>(o, row, v, vec16{0, 0, 0, 0});
     return;
   }
   const float c = LOG2E / r.temperature;
@@ -615,18 +615,18 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void l
     for (int u = 0; u < AGAIN; ++u) {
       const int w = v + u * W + threadIdx.x;
       as_loaded(a[u]);
-      store_vector<DT, true>(o, row, w, grad_vector<DT>(a[u], target - entry_of<DT>(row, w), g));
+      store_vector<DT>(o, row, w, grad_vector<DT>(a[u], target - entry_of<DT>(row, w), g));
     }
   }
   for (; v < row.count; v += W) {
     const int w = v + threadIdx.x;
-    store_vector<DT, true>(o, row, w, grad_vector<DT>(load_vector<DT>(x, row, w), target - entry_of<DT>(row, w), g));
+    store_vector<DT>(o, row, w, grad_vector<DT>(load_vector<DT>(x, row, w), target - entry_of<DT>(row, w), g));
   }
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     const int w = u * W + threadIdx.x;
     as_loaded(q[u]);
-    store_vector<DT, true>(o, row, w, grad_vector<DT>(q[u], target - entry_of<DT>(row, w), g));
+    store_vector<DT>(o, row, w, grad_vector<DT>(q[u], target - entry_of<DT>(row, w), g));
   }
 }
 
