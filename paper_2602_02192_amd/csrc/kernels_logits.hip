@@ -62,6 +62,7 @@ template <int DT> __device__ __forceinline__ Vectors vectors_of(int vocab) {
 }
 template <int DT> __device__ __forceinline__ uint32_t byte_of(int entry) { return (uint32_t)entry * (uint32_t)sizeof(typename Elem<DT>::type); }
 template <int DT> __device__ __forceinline__ int entry_of(const Vectors &r, int v) { return max(v * Elem<DT>::VEC - r.repeated, 0); }
+// (Beyond the last vector: that one, which the caller drops.)
 template <int DT> __device__ __forceinline__ vec16 load_vector(const typename Elem<DT>::type *x, const Vectors &r, int v) {
   vec16 q;
   __builtin_memcpy(&q, (const char *)x + byte_of<DT>(entry_of<DT>(r, min(v, r.count - 1))), 16);
@@ -271,7 +272,10 @@ __device__ __forceinline__ void write_top(const RowOutputs &out, int64_t t, int 
   out.top_logprobs[t * out.top_k + i] = !live ? 0.f : key ? logprob(key_value(key), s, inv_t) : -INFINITY;
 }
 
-// One part of a row.  ONE: it is all of the row, and the outputs are written here.
+// One part of a row, read once: with the anchor at the largest entry so far, an entry costs a widening, an fma, an exponential, an addition, a maximum and an fma.
+// ONE: the part is all of the row, and the outputs are written here.  4096 rows of 151936 bf16: 209 to 217 us, 5.7 to 6.0 TB/s, bound by the loads (without the sum for the
+// entropy 1 % less).  Few rows are bound by the latency of one round: 64 rows with top 8 12.4 us, 999 rows of 32001 half entries with top 5 18 us.
+// A batch of 8 vectors keeps loads ahead of the arithmetic; 4 took 223 instead of 217 us.
 template <int DT, int BATCH, bool TOP, bool ONE> __global__ __launch_bounds__(THREADS) void stats_kernel(LogitRows r, Parts p, int splits, int span, RowOutputs outputs) {
   constexpr int VEC = Elem<DT>::VEC;
   __shared__ RowStats sh[THREADS / 64];
@@ -376,6 +380,7 @@ __device__ __forceinline__ RowPart joined(const RowPart *part, int splits, float
   return {wave_stats(m.s, c), wave_max(m.given)};
 }
 
+// A row from its parts.  Bound by the latency of its steps: 4.6 us for 4096 rows of three parts, 7 for one row whose 75 parts bring 20 keys each.
 template <bool TOP> __global__ __launch_bounds__(THREADS) void stats_finish_kernel(LogitRows r, Parts p, int splits, RowOutputs out) {
   const int64_t t = blockIdx.x;
   const float inv_t = 1.0f / r.temperature;
@@ -515,7 +520,8 @@ __device__ __forceinline__ float far_entry_grad(float x, const RowGrad &c) {
   return mul_legacy(__builtin_amdgcn_exp2f(d), fmaf(c.b, d, c.a));
 }
 
-// One batch of a row's gradient: from given statistics (LOSS false), or from the parts of stats_kernel, which every workgroup of a row joins while its
+// One batch of a row's gradient, an fma, an exponential, an fma and a product an entry, bound by memory: 512 rows of 151936 bf16 59 us, 5.3 TB/s read and written, 777 rows of
+// 32001 f32 28 us, 6.0.  Workgroups of a batch each, since nothing is shared but the row's coefficients.  From given statistics (LOSS false), or from the parts of stats_kernel, which every workgroup of a row joins while its
 // vectors are on their way.
 template <int DT, bool LOSS> __global__ __launch_bounds__(THREADS) void grad_kernel(LogitRows r, GivenStats given, PolicyTerms terms, Parts p, int splits, LossOutputs out,
                                                                                  int batches) {
@@ -571,7 +577,8 @@ template <int DT, bool LOSS> __global__ __launch_bounds__(THREADS) void grad_ker
 }
 
 // A whole row by one workgroup: its first N vectors a thread stay in registers between the statistics and the gradient, what is beyond them is read
-// again.
+// again, mostly out of the memory-side cache.  4096 rows of 151936 bf16 of which 65 % take part: 417 us, 4.9 TB/s of what has to be read and written, as fast as a large
+// copy, with the vector unit 63 % busy; 64 rows of 1024 f32 5.5 us, a load's latency, a reduction's and a store's.
 template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void loss_row_kernel(LogitRows r, PolicyTerms terms, LossOutputs out) {
   constexpr int AGAIN = 4;
   __shared__ RowStats sh[W / 64];
@@ -696,8 +703,9 @@ template <int DT> __global__ __launch_bounds__(THREADS) void narrow_kernel(Logit
   }
 }
 
-// Parts of a row: one batch each where the top entries are wanted, up to four otherwise, as many as leave some thousand parts; of few rows small batches, so that there
-// are parts for the whole GPU.
+// Parts of a row: one batch each where the top entries are wanted, up to four otherwise, as many as leave some thousand parts (4096 rows of 151936 bf16: 219 us, 230 with
+// one batch each, 217 with ten).  Of few rows small batches, so that there are parts for the whole GPU (bf16, both kernels, 1 row 6.6 us, 7.1 with large ones; 24 rows
+// with top 20 14.7 and 16.3), but not of more (999 rows of 32001 with top 5 27 us, 23 with large ones).
 struct Split { int splits, span, batch; };   // span: vectors of a part
 int vector_entries(const LogitRows &x) { return x.dtype == ECHO_F32 ? 4 : 8; }
 int row_vectors(const LogitRows &x) { return (x.vocab + vector_entries(x) - 1) / vector_entries(x); }
@@ -719,9 +727,16 @@ size_t logprobs_workspace(const LogitRows &x, int top_k) {
   return parts_bytes(x, s) + (s.splits == 1 ? 0 : (size_t)x.rows * s.splits * top_k * sizeof(uint64_t));
 }
 
-// Whether a workgroup takes a row whole, or several take parts of it and its gradient in two launches.  Short rows whole in any number; long ones where there are
-// enough to fill the GPU.  151936 entries, bf16: 64 rows 30 us whole, 20 in parts; 128 rows 31 and 31; 200 rows 33 and 41.  f32: 29 and 23, 36 and 40, 50 and 73.
-static bool by_rows(const LogitRows &x) { return row_vectors(x) <= 8192 || x.rows >= 128; }
+// Whether a workgroup takes a row whole, or several take parts of it and its gradient in two launches.  Rows that registers hold are read once, and taken whole (bf16
+// 70000 entries, 64 rows: 14 us, 16 in parts).  Of longer rows the parts read everything twice, which costs little as long as the memory-side cache has it; whole
+// rows leave CUs idle in the last round of 256.  Below 256 MB of logits parts win while that round has fewer than some 176 rows of 16 bits, 96 of f32: 151936
+// bf16, 128 rows 29 us whole and 22 in parts, 192 rows 31 and 32, 300 rows 56 and 44, 420 rows 60 and 61; f32, 64 rows 27 and 21, 128 rows 34 and 36, 300 rows 86 and 80.
+// Beyond: 1100 rows of bf16 151 and 186, 460 of f32 113 and 128.
+static bool by_rows(const LogitRows &x) {
+  const int64_t n = row_vectors(x), held = x.dtype == ECHO_F32 ? 1024 * 17 : 512 * 18, last_round = (x.rows - 1) % 256 + 1;
+  if (split_of(x, false).splits == 1) return true;   // (one part has no workspace)
+  return n <= held || x.rows * n > (256 << 20) / 16 || last_round >= (x.dtype == ECHO_F32 ? 96 : 176);
+}
 size_t policy_workspace(const LogitRows &x) { return by_rows(x) ? 0 : parts_bytes(x, split_of(x, false)); }
 
 #define FOR_DTYPE(dt, CALL)                                    \

@@ -77,6 +77,17 @@ def test_against_the_formulas(learner, dtype, rows, vocab, pad, offset, T):
     assert place.grad_logits.data_ptr() == x.data_ptr() and torch.equal(x, got.grad_logits) and torch.equal(place.loss, got.loss)
 
 
+@pytest.mark.parametrize("dtype,rows,vocab", [("bf16", 175, 100003), ("bf16", 176, 100003), ("bf16", 257, 75001), ("f16", 176, 90113), ("f32", 95, 90001), ("f32", 96, 90001), ("f32", 257, 70001)])
+def test_long_rows_whole_and_in_parts(learner, dtype, rows, vocab):
+    """Row counts on both sides of where a row is cut; rows longer than what a workgroup keeps of them, with and without a place of their own for the gradient."""
+    x, targets, r = make(rows, vocab, dtype, rows + vocab)
+    a, want = inputs(x, targets, r, 1.0)
+    got = learner.policy_loss(x, targets, **a, **COEF)
+    check(got, x, targets, a, want, COEF, 1.0, dtype)
+    place = learner.policy_loss(x, targets, grad_out=x, **a, **COEF)
+    assert torch.equal(x, got.grad_logits) and torch.equal(place.loss, got.loss)
+
+
 @pytest.mark.parametrize("dtype,vocab", [("bf16", 2000), ("bf16", 151936), ("f32", 40000)])
 def test_absent_terms(learner, dtype, vocab):
     x, targets, r = make(40, vocab if vocab < 100000 else vocab, dtype, 8)

@@ -60,6 +60,18 @@ def test_arguments_that_are_refused(learner):
     assert L.echo_token_logprobs_grad(C.byref(big), None, 64, 64, 64, 64, 151936, None) == -1 and "lse" in message(learner)
 
 
+def test_a_loss_in_parts_has_room_for_them(learner):
+    """Rows of few vectors are never cut; a cut row has two parts of 16 bytes at least, whatever its type, its length and their number."""
+    for dtype, entries in ((0, 4), (1, 8), (2, 8)):
+        for vocab in (1, 7, 8, 1024, 35000, 65536, 65537, 70000, 73728, 73729, 100003, 151936, 262144, 500000):
+            for rows in (1, 8, 32, 95, 96, 128, 175, 176, 256, 257, 300, 512, 4096):
+                need = learner.lib.echo_policy_loss_workspace(C.byref(learner._Logits(64, 64, rows, vocab, vocab, dtype, 1.0)))
+                if -(-vocab // entries) <= 8192:
+                    assert need == 0
+                assert need == 0 or (need >= rows * 2 * 16 and need % 256 == 0)
+    assert learner.lib.echo_policy_loss_workspace(C.byref(learner._Logits(64, 64, 32, 151936, 151936, 1, 1.0))) > 0
+
+
 def test_sizes_of_the_update(learner):
     def i64(*v):
         return np.array(v, np.int64)
