@@ -64,7 +64,7 @@ const char *wrong_pointers(const echo_logits *x) {
   if (misaligned(x->targets, 4)) return "targets are not aligned to their elements";
   return nullptr;
 }
-LogitRows rows_of(const echo_logits *x) { return {x->logits, x->targets, x->rows, x->row_stride, x->vocab, x->dtype, x->temperature}; }
+LogitRows rows_of(const echo_logits *x) { return {x->logits, x->targets, x->rows, x->row_stride, x->vocab, x->dtype, x->temperature, nullptr}; }
 
 bool any_misaligned4(std::initializer_list<const void *> ps) {
   for (const void *p : ps)
@@ -170,9 +170,10 @@ int echo_policy_loss(const echo_logits *x, const float *advantages, const float 
     if (o->kl_coef != 0.f && !ref_logprobs) return refuse(ECHO_EINVAL, "kl_coef = %g needs ref_logprobs", (double)o->kl_coef);
     if (any_misaligned4({advantages, old_logprobs, weights, sampler_logprobs, ref_logprobs, out_loss, out_logprobs, out_entropy}))
       return refuse(ECHO_EINVAL, "an array is not aligned to its elements");
-    const LogitRows r = rows_of(x);
+    LogitRows r = rows_of(x);
+    r.weights = weights;
     if (const char *why = wrong_workspace(workspace, workspace_bytes, policy_workspace(r))) return refuse(ECHO_ENOMEM, "%s", why);
-    const PolicyTerms p = {advantages, old_logprobs, weights, sampler_logprobs, ref_logprobs, (float)(1.0 - (double)o->clip_low), (float)(1.0 + (double)o->clip_high),
+    const PolicyTerms p = {advantages, old_logprobs, sampler_logprobs, ref_logprobs, (float)(1.0 - (double)o->clip_low), (float)(1.0 + (double)o->clip_high),
                            o->ratio_cap, o->sampler_cap, o->kl_coef, o->entropy_coef};
     return queue([&] { launch_policy_loss(r, p, out_loss, out_logprobs, out_entropy, out_grad, grad_stride, workspace, (hipStream_t)stream); });
   });

@@ -98,7 +98,7 @@ template <int DT> __device__ __forceinline__ vec16 own_entries(vec16 q, int repe
 }
 
 __device__ __forceinline__ bool row_live(const LogitRows &r, int64_t t) {
-  return !r.targets || (uint32_t)r.targets[t] < (uint32_t)r.vocab;
+  return (!r.weights || r.weights[t] != 0.f) && (!r.targets || (uint32_t)r.targets[t] < (uint32_t)r.vocab);
 }
 
 // Order of the entries of a row: by logit, then by falling index; 0 is below every entry.
@@ -462,8 +462,8 @@ template <int DT> __device__ __forceinline__ vec16 grad_vector(const vec16 &q, i
 }
 
 struct TokenLoss { float loss, logprob, g, h; };
-__device__ TokenLoss token_loss(const PolicyTerms &p, int64_t t, float lp, float H) {
-  const float w = p.weights ? p.weights[t] : 1.f, A = p.advantages[t], old = p.old_logprobs[t];
+__device__ TokenLoss token_loss(const LogitRows &r, const PolicyTerms &p, int64_t t, float lp, float H) {
+  const float w = r.weights ? r.weights[t] : 1.f, A = p.advantages[t], old = p.old_logprobs[t];
   const float ratio = expf(lp - old), trust = p.sampler ? fminf(expf(old - p.sampler[t]), p.sampler_cap) : 1.f;
   const float free = fminf(ratio, p.ratio_cap) * A, held = fminf(fmaxf(ratio, p.lo), p.hi) * A;
   float kl = 0.f, kl_slope = 0.f;
@@ -475,16 +475,13 @@ __device__ TokenLoss token_loss(const PolicyTerms &p, int64_t t, float lp, float
   const float slope = free <= held && ratio < p.ratio_cap ? A * ratio : 0.f;
   return {w * (-trust * fminf(free, held) + kl - p.entropy * H), lp, w * (kl_slope - trust * slope), -p.entropy * w};
 }
-__device__ __forceinline__ bool token_live(const LogitRows &r, const PolicyTerms &p, int64_t t) {
-  return row_live(r, t) && (!p.weights || p.weights[t] != 0.f);
-}
 
 struct LossOutputs { float *loss, *logprobs, *entropy; void *grad; int64_t stride; };
 
 // Loss of a row from its statistics; its outputs by the thread that `writes`.
 __device__ __forceinline__ RowGrad finish_loss(const LogitRows &r, const PolicyTerms &p, const LossOutputs &out, int64_t t, const RowStats &s, float given, bool writes) {
   const float inv_t = 1.0f / r.temperature, H = stats_entropy(s);
-  const TokenLoss l = token_loss(p, t, logprob(given, s, inv_t), H);
+  const TokenLoss l = token_loss(r, p, t, logprob(given, s, inv_t), H);
   if (writes) {
     if (out.loss) out.loss[t] = l.loss;
     if (out.logprobs) out.logprobs[t] = l.logprob;
@@ -532,9 +529,7 @@ template <int DT, bool LOSS> __global__ __launch_bounds__(THREADS) void grad_ker
   const bool first = blockIdx.x % (uint32_t)batches == 0;
   const auto *x = (const typename Elem<DT>::type *)r.x + t * r.stride;
   auto *o = (typename Elem<DT>::type *)out.grad + t * out.stride;
-  bool live;
-  if constexpr (LOSS) live = token_live(r, terms, t); else live = row_live(r, t) && given.lse[t] != -INFINITY;
-  if (!live) {
+  if (!row_live(r, t) || (!LOSS && given.lse[t] == -INFINITY)) {
     if (LOSS && first && threadIdx.x == 0) no_loss(out, t);
 #pragma unroll
     for (int u = 0; u < BATCH; ++u)
@@ -586,7 +581,7 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void l
   const auto *x = (const typename Elem<DT>::type *)r.x + t * r.stride;
   auto *o = (typename Elem<DT>::type *)out.grad + t * out.stride;
   const Vectors row = vectors_of<DT>(r.vocab);
-  if (!token_live(r, terms, t)) {
+  if (!row_live(r, t)) {
     if (threadIdx.x == 0) no_loss(out, t);
     if (!out.grad) return;
     for (int v = threadIdx.x; v < row.count; v += W) store_vector<DT>(o, row, v, vec16{0, 0, 0, 0});
@@ -640,7 +635,7 @@ template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void l
 // The loss alone.
 __global__ __launch_bounds__(64) void loss_finish_kernel(LogitRows r, PolicyTerms terms, Parts p, int splits, LossOutputs out) {
   const int64_t t = blockIdx.x;
-  if (!token_live(r, terms, t)) {
+  if (!row_live(r, t)) {
     if (threadIdx.x == 0) no_loss(out, t);
     return;
   }
@@ -656,7 +651,6 @@ template <int DT> __global__ __launch_bounds__(THREADS) void narrow_kernel(Logit
   const float inv_t = 1.0f / r.temperature, c = LOG2E / r.temperature;
   const int target = r.targets ? r.targets[t] : -1;
   bool live = row_live(r, t);
-  if (loss) live = token_live(r, terms, t);
   RowStats s = {-INFINITY, 0.f, 0.f};
   float v[8];
 #pragma unroll

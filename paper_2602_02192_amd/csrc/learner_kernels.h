@@ -11,6 +11,7 @@ struct LogitRows {
   int64_t rows, stride;
   int32_t vocab, dtype;
   float temperature;
+  const float *weights;     // nullable; a row of weight 0 takes no part
 };
 
 struct RowOutputs {
@@ -21,7 +22,7 @@ struct RowOutputs {
 };
 
 struct PolicyTerms {
-  const float *advantages, *old_logprobs, *weights, *sampler, *ref;   // weights, sampler, ref nullable
+  const float *advantages, *old_logprobs, *sampler, *ref;   // sampler, ref nullable
   float lo, hi, ratio_cap, sampler_cap, kl, entropy;                  // lo, hi: bounds of the clipped ratio
 };
 
