@@ -57,7 +57,7 @@ int echo_token_logprobs(const echo_logits *x, int32_t top_k, float *out_logprobs
  *   out[t][j] = (grad_logprobs (1[j = target] - p_j) - grad_entropy p_j (ln p_j + entropy)) / T,   p_j = exp(x_j / T - lse)
  * lse and entropy device f32 [rows], as echo_token_logprobs gave them.  grad_entropy may be NULL (the entropy is not read then), and so may
  * grad_logprobs, but not both; without targets every row takes part and grad_logprobs must be NULL.  out: device, the logits' type, rows out_stride elements apart; may be the logits themselves (same stride).  Every row is
- * written, one that takes no part with 0. */
+ * written, one that takes no part with 0.  p_j carries the rounding of lse, 2^-24 of its size. */
 int echo_token_logprobs_grad(const echo_logits *x, const float *lse, const float *entropy, const float *grad_logprobs, const float *grad_entropy,
                              void *out, int64_t out_stride, void *stream);
 

@@ -572,7 +572,7 @@ template <int DT, bool LOSS> __global__ __launch_bounds__(THREADS) void grad_ker
 }
 
 // A whole row by one workgroup: its first N vectors a thread stay in registers between the statistics and the gradient, what is beyond them is read
-// again, mostly out of the memory-side cache.  4096 rows of 151936 bf16 of which 65 % take part: 417 us, 4.9 TB/s of what has to be read and written, as fast as a large
+// again, mostly out of the memory-side cache.  4096 rows of 151936 bf16 of which 65 % take part: 402 to 419 us, 4.9 to 5.1 TB/s of what has to be read and written, as fast as a large
 // copy, with the vector unit 63 % busy; 64 rows of 1024 f32 5.5 us, a load's latency, a reduction's and a store's.
 template <int DT, int W, int N> __global__ __launch_bounds__(W, 1024 / W) void loss_row_kernel(LogitRows r, PolicyTerms terms, LossOutputs out) {
   constexpr int AGAIN = 4;
