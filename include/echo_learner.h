@@ -35,8 +35,8 @@ enum { ECHO_F16 = 2, ECHO_E4M3 = 3 };
 typedef struct {
   const void *logits;      /* device [rows, row_stride] */
   const int32_t *targets;  /* device [rows]: the given token of each row */
-  int64_t rows, row_stride; /* row_stride >= vocab */
-  int32_t vocab;
+  int64_t rows, row_stride; /* rows * ceil(vocab / 8192) < 2^24; row_stride >= vocab */
+  int32_t vocab;           /* 1 .. 2^28 */
   int32_t dtype;           /* ECHO_F32, ECHO_BF16 or ECHO_F16 */
   float temperature;       /* > 0, 1 / temperature finite */
 } echo_logits;
@@ -56,8 +56,8 @@ int echo_token_logprobs(const echo_logits *x, int32_t top_k, float *out_logprobs
 /* Gradient of sum_t grad_logprobs[t] logprobs[t] + grad_entropy[t] entropy[t] with respect to the logits:
  *   out[t][j] = (grad_logprobs (1[j = target] - p_j) - grad_entropy p_j (ln p_j + entropy)) / T,   p_j = exp(x_j / T - lse)
  * lse and entropy device f32 [rows], as echo_token_logprobs gave them.  grad_entropy may be NULL (the entropy is not read then), and so may
- * grad_logprobs, but not both; without targets every row takes part and grad_logprobs must be NULL.  out: device, the logits' type, rows out_stride elements apart; may be the logits themselves (same stride).  Every row is
- * written, one that takes no part with 0.  p_j carries the rounding of lse, 2^-24 of its size. */
+ * grad_logprobs, but not both; without targets every row takes part and grad_logprobs must be NULL.  out: device, the logits' type, rows out_stride elements apart;
+ * the logits themselves (same stride) or memory that they have no part in.  Every row is written, one that takes no part with 0.  p_j carries the rounding of lse, 2^-24 of its size. */
 int echo_token_logprobs_grad(const echo_logits *x, const float *lse, const float *entropy, const float *grad_logprobs, const float *grad_entropy,
                              void *out, int64_t out_stride, void *stream);
 

@@ -49,9 +49,10 @@ const char *wrong_logits(const echo_logits *x) {
   if (!x) return "logits description is NULL";
   const size_t e = element_bytes(x->dtype);
   if (!e) return "logits must be ECHO_F32, ECHO_BF16 or ECHO_F16";
-  if (x->rows < 0 || x->rows > INT32_MAX) return "rows must lie in 0 .. 2^31 - 1";
+  if (x->rows < 0) return "rows must not be negative";
   if (x->vocab < 1 || x->vocab > 1 << 28) return "vocab must lie in 1 .. 2^28";
-  if (x->rows * ((x->vocab + 8191) / 8192) > INT32_MAX) return "rows * vocab exceeds what one call takes (2^44)";
+  // A launch has less than 2^32 threads: 256 for every 8192 entries of a row at most, and 512 or 1024 for a row of two or five times as many.
+  if (x->rows > ((1 << 24) - 1) / ((x->vocab + 8191) / 8192)) return "rows * ceil(vocab / 8192) must be less than 2^24";
   if (x->row_stride < x->vocab) return "row_stride is less than vocab";
   if (x->rows > 0 && x->row_stride > INT64_MAX / 16 / x->rows) return "rows * row_stride is out of range";
   if (!(x->temperature > 0.f) || !std::isfinite(x->temperature) || !std::isfinite(2.0f / x->temperature)) return "temperature must be positive, finite, and its reciprocal too";

@@ -325,6 +325,8 @@ class AdamW:
             raise ValueError(f"states must be float32 or float8_e4m3fn, got {state_dtype}")
         self.params, self.snapshot = list(params), None if snapshot is None else list(snapshot)
         self.lr, self.betas, self.eps, self.weight_decay, self.max_norm, self.seed, self.steps = lr, betas, eps, weight_decay, max_norm, seed, 0
+        if not self.params:
+            raise ValueError("no params")
         n, dev = state_numel(self.params), self.params[0].device
         self.m, self.v = (torch.zeros(n, dtype=torch.uint8 if state_dtype != torch.float32 else torch.float32, device=dev).view(state_dtype) for _ in range(2))
         self.m_scale, self.v_scale = (torch.zeros(n // BLOCK, device=dev) for _ in range(2)) if state_dtype != torch.float32 else (None, None)

@@ -60,6 +60,24 @@ def test_arguments_that_are_refused(learner):
     assert L.echo_token_logprobs_grad(C.byref(big), None, 64, 64, 64, 64, 151936, None) == -1 and "lse" in message(learner)
 
 
+@pytest.mark.parametrize("rows,vocab,taken", [((1 << 24) - 1, 8, True), (1 << 24, 8, False), (1 << 24, 8192, False), ((1 << 23) - 1, 8193, True), (1 << 23, 8193, False),
+                                              ((1 << 24) - 1, 1, True), (1 << 24, 1, False), (511, 1 << 28, True), (512, 1 << 28, False)])
+def test_logits_of_more_workgroups_than_a_launch_has(learner, rows, vocab, taken):
+    """A launch has less than 2^32 threads; what would need more is refused before anything is queued, and has no workspace."""
+    x = learner._Logits(None, None, rows, vocab, vocab, 1, 1.0)    # (no logits: what is taken is refused for that)
+    for call in (lambda: learner.lib.echo_token_logprobs(C.byref(x), 0, None, 64, 64, None, None, 256, 1 << 60, None),
+                 lambda: learner.lib.echo_token_logprobs_grad(C.byref(x), 64, 64, None, 64, 64, vocab, None),
+                 lambda: learner.lib.echo_policy_loss(C.byref(x), 64, 64, None, None, None, C.byref(learner._LossOpts(0.2, 0.2, 4, 2, 0, 0)), 64, 64, 64, 64, vocab, 256, 1 << 60, None)):
+        assert call() == -1 and ("logits are NULL" if taken else "2^24") in message(learner)
+    if not taken:
+        assert learner.lib.echo_token_logprobs_workspace(C.byref(x), 0) == 0 and learner.lib.echo_policy_loss_workspace(C.byref(x)) == 0
+
+
+def test_no_parameters(learner):
+    with pytest.raises(ValueError, match="no params"):
+        learner.AdamW([], 1e-3)
+
+
 def test_a_loss_in_parts_has_room_for_them(learner):
     """Rows of few vectors are never cut; a cut row has two parts of 16 bytes at least, whatever its type, its length and their number."""
     for dtype, entries in ((0, 4), (1, 8), (2, 8)):
