@@ -2,7 +2,8 @@
 alternatives, the policy loss with its gradient, the norm of many gradients and the AdamW step that ends in a snapshot.
 
 Argument marshalling only: the arithmetic is in the library's HIP kernels.  Calls are queued on the current stream of the
-tensors' GPU and do not wait; the usual rules of torch for tensors that other streams use apply to them.  Arguments that the library
+tensors' GPU and do not wait; the usual rules of torch for tensors that other streams use apply to them.  Tensors that a call writes count as
+changed in place (a backward pass that needs their old values raises).  Arguments that the library
 refuses raise echo.EchoError, tensors that it could not be handed (another type, device or layout) ValueError."""
 from __future__ import annotations
 
@@ -12,6 +13,8 @@ import struct
 from typing import NamedTuple, Optional, Sequence
 
 import torch
+from torch.autograd.function import once_differentiable
+from torch.autograd.graph import increment_version
 
 from .echo import ECHO_BF16, ECHO_F32, EchoError, lib
 
@@ -175,6 +178,7 @@ class _Differentiable(torch.autograd.Function):
         return tuple(r)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g, h, *_):
         logits, targets, lse, entropy = ctx.saved_tensors
         if g is None and h is None:
@@ -199,9 +203,11 @@ def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor], l
     `out` may be the logits themselves."""
     x, rows, gpu = _logits(logits, targets, temperature)
     a = [_vector(t, n, rows, gpu) for t, n in ((lse, "lse"), (entropy, "entropy"), (grad_logprobs, "grad_logprobs"), (grad_entropy, "grad_entropy"))]
-    out = _grad_like(logits, out)
-    _call(gpu, lib.echo_token_logprobs_grad, C.byref(x), *a, out.data_ptr(), _matrix(out, "out")[2])
-    return out
+    grad = _grad_like(logits, out)
+    _call(gpu, lib.echo_token_logprobs_grad, C.byref(x), *a, grad.data_ptr(), _matrix(grad, "out")[2])
+    if out is not None:
+        increment_version(out)
+    return grad
 
 
 def _grad_like(logits, out):
@@ -242,6 +248,8 @@ def policy_loss(logits: torch.Tensor, targets: torch.Tensor, advantages: torch.T
     need = lib.echo_policy_loss_workspace(xp)
     ws = _workspace(need, logits)
     _call(gpu, lib.echo_policy_loss, xp, *a, C.byref(o), loss.data_ptr(), logprobs.data_ptr(), entropy.data_ptr(), _addr(grad), stride, _addr(ws), need)
+    if grad_out is not None:
+        increment_version(grad_out)
     return PolicyLoss(loss, logprobs, entropy, grad)
 
 
@@ -265,7 +273,7 @@ def _same(tensors: Sequence[torch.Tensor], name: str, dtypes):
 def grad_norm(grads: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Euclidean norm of all the gradients together: a float32 tensor of one value on their GPU (`out`, or a new one)."""
     addresses, numel, dtype, gpu = _same(grads, "grads", (torch.float32, torch.bfloat16, torch.float16))
-    like, n = grads[0], len(grads)
+    like, n, given = grads[0], len(grads), out
     if out is None:
         out = torch.empty((), dtype=torch.float32, device=like.device)
     elif out.dtype is not torch.float32 or out.numel() != 1 or out.get_device() != gpu:
@@ -273,6 +281,8 @@ def grad_norm(grads: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None)
     need = lib.echo_grad_norm_workspace(numel, n)
     ws = _workspace(need, like)
     _call(gpu, lib.echo_grad_norm, addresses, numel, n, _DTYPE[dtype], out.data_ptr(), _addr(ws), need)
+    if given is not None:
+        increment_version(given)
     return out
 
 
@@ -313,6 +323,7 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     a = _AdamW(pa, ga, sa, numel, struct.pack(f"{count}d", *decays), ma, va, msa, vsa, _addr(norm), lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, max_norm,
                count, _DTYPE[ptype], _DTYPE[gtype], _DTYPE[states])
     _call(gpu, lib.echo_adamw_step, C.byref(a))
+    increment_version([*params, *(snapshot or ()), m, v, *(() if m_scale is None else (m_scale, v_scale))])
 
 
 class AdamW:

@@ -328,3 +328,31 @@ def test_refusals(learner):
     with pytest.raises(ValueError):
         learner.token_logprobs_grad(x, targets, z, z, z, out=torch.empty(4, 99, device="cuda"))
 
+
+def test_no_second_derivative(learner):
+    """Refused, not left out of the sum that it belongs to."""
+    x, targets, r = make(5, 40, "f32", 3)
+    x = x.clone().requires_grad_()
+    first, = torch.autograd.grad((learner.token_logprobs(x, targets).logprobs ** 2).sum() + (x ** 3).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        first.sum().backward()
+
+
+def test_what_is_written_in_place_counts_as_changed(learner):
+    """A backward pass that still needs the old values is refused by torch, as after its own operations in place."""
+    x, targets, r = make(5, 40, "f32", 4)
+    z, w = torch.zeros(5, device="cuda"), torch.ones(5, 40, device="cuda", requires_grad=True)
+    for write in (lambda y: learner.policy_loss(y, targets, z, z, grad_out=y),
+                  lambda y: learner.token_logprobs_grad(y, targets, z, None, z, out=y),
+                  lambda y: learner.adamw_step([y], [torch.ones_like(y)], torch.zeros(256, device="cuda"), torch.zeros(256, device="cuda"), step=1, lr=0.1)):
+        y = x.clone().contiguous()
+        later = (y * w).sum()
+        write(y)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            later.backward()
+    p, g, s, out = (torch.zeros(300, device="cuda") for _ in range(4))
+    m, v, short = torch.zeros(512, device="cuda"), torch.zeros(512, device="cuda"), torch.zeros(300, dtype=torch.bfloat16, device="cuda")
+    norm = torch.zeros((), device="cuda")
+    learner.grad_norm([g], out=norm)
+    learner.adamw_step([p], [g], m, v, step=1, lr=0.1, snapshot=[short])
+    assert all(t._version > 0 for t in (norm, p, m, v, short)) and g._version == 0
